@@ -1,0 +1,280 @@
+"""Python binding of the 8-bit integer operators of libcurvefp (argument marshalling only).
+
+The functions carry the names of the C ABI in ``include/cfint8.h``: quantization with one fp32 scale
+for each line, reconstruction, the product of such codes, and a mixture-of-experts layer for a few
+tokens with such weights.  Tensors are checked like ``curvefp``'s: device, dtype, layout and size, a
+failed check raising ValueError before anything reaches the library.
+
+Matrices of codes are 2-D int8 tensors whose row stride is a multiple of 16 bytes; a matrix of odd
+width is a view of a wider buffer (``codes_buffer``).
+"""
+
+import ctypes
+from typing import Optional, Tuple
+
+import torch
+
+from . import curvefp as _cf
+from .curvefp import DTYPES, CurveFPError, _check, _matrix, _on_gpu, _source_arg, _stream
+
+_fn = None
+
+
+def lib() -> ctypes.CDLL:
+    """libcurvefp.so with this header's signatures."""
+    global _fn
+    if _fn is None:
+        L = _cf.lib()
+        P, I, I64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+        L.cfint8_quantize_workspace_bytes.argtypes = [I64, I64, I]
+        L.cfint8_quantize_workspace_bytes.restype = I64
+        L.cfint8_quantize.argtypes = [P, I, I64, I64, I64, I, P, P, I64, P, P, I64, P]
+        L.cfint8_quantize.restype = I
+        L.cfint8_dequantize.argtypes = [P, I64, P, I64, I64, P, I, I64, P]
+        L.cfint8_dequantize.restype = I
+        L.cfint8_gemm_workspace_bytes.argtypes = [I64, I64, I64, I]
+        L.cfint8_gemm_workspace_bytes.restype = I64
+        L.cfint8_gemm.argtypes = [P, I64, P, P, I64, I, P, P, I64, I64, I64, P, I, I64, P, I64, P]
+        L.cfint8_gemm.restype = I
+        L.cfint8_moe_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
+        L.cfint8_moe_workspace_bytes.restype = I64
+        L.cfint8_moe.argtypes = [P, I, I64, I64, I64, P, I64, P, P, P, P, I64, I64, I, P, P, I64, P, P, P, I64, P]
+        L.cfint8_moe.restype = I
+        _fn = L
+    return _fn
+
+
+# ---------------------------------------------------------------- argument checks
+
+def _readable(what: str, name: str, t: torch.Tensor, rows: int, cols: int):
+    """The last of the rows is readable up to the next multiple of 16 bytes (the others end in the next one)."""
+    es = t.element_size()
+    if (cols * es) % 16 == 0 or t.device.type == "meta":
+        return
+    end = (t.storage_offset() + (rows - 1) * t.stride(0)) * es + -(-cols * es // 16) * 16
+    if t.untyped_storage().nbytes() < end:
+        raise ValueError(f"{what}: {name}'s last row must be readable up to a multiple of 16 bytes "
+                         f"(a view of a wider buffer)")
+
+
+def _codes(what: str, name: str, t: torch.Tensor, rows: int, cols: int):
+    """A matrix of codes that is read."""
+    _matrix(what, name, t, rows, cols, (torch.int8,))
+    _readable(what, name, t, rows, cols)
+
+
+def _vector(what: str, name: str, t: torch.Tensor, n: int, dtype=torch.float32):
+    """A contiguous vector (any shape) of at least n values."""
+    if t.dtype != dtype:
+        raise ValueError(f"{what}: {name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be contiguous")
+    if t.numel() < n:
+        raise ValueError(f"{what}: {name} holds {t.numel()} values, the call needs {n}")
+
+
+def _bytes(what: str, fn, *args) -> int:
+    n = fn(*args)
+    if n < 0:
+        raise CurveFPError(int(n), what)
+    return int(n)
+
+
+def _scratch(what, workspace, need: int, device, stream):
+    """(pointer, bytes) of the workspace, allocated here when not given."""
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None and device.type == "cuda":
+            workspace.record_stream(stream)      # its memory goes back when this call returns
+    have = workspace.numel() * workspace.element_size()
+    if not workspace.is_contiguous() or have < need:
+        raise ValueError(f"{what}: workspace must be contiguous and hold {need} bytes, it holds {have}")
+    return workspace.data_ptr(), have, workspace
+
+
+def _ld(t: torch.Tensor, rows: int, cols: int) -> int:
+    """Leading dimension of a matrix with 16-byte aligned rows; a single row has none of its own."""
+    if rows > 1:
+        return t.stride(0)
+    per = 16 // t.element_size()
+    return -(-cols // per) * per
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def codes_buffer(rows: int, k: int, device) -> torch.Tensor:
+    """An uninitialised [rows, k] matrix of codes with rows of whole 16-byte pieces."""
+    ld = -(-k // 16) * 16
+    t = torch.empty((rows, ld), dtype=torch.int8, device=device)
+    return t if ld == k else t[:, :k]
+
+
+# ---------------------------------------------------------------- entry points
+
+def cfint8_quantize_workspace_bytes(rows: int, cols: int, block_axis: int = 1) -> int:
+    return _bytes("cfint8_quantize_workspace_bytes", lib().cfint8_quantize_workspace_bytes, rows, cols, block_axis)
+
+
+def cfint8_quantize(src: torch.Tensor, block_axis: int = 1, mul: Optional[torch.Tensor] = None,
+                    codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Codes and scales of a 2-D fp32/bf16 tensor: block_axis=1, a scale for each row, codes
+    [rows, cols]; block_axis=0, a scale for each column, codes [cols, rows].  mul: fp32 factors along
+    the quantized axis, multiplied in first."""
+    what = "cfint8_quantize"
+    ts = [("src", src)]
+    for name, t in (("mul", mul), ("codes", codes), ("scales", scales), ("workspace", workspace)):
+        if t is not None:
+            ts.append((name, t))
+    _on_gpu(what, ts, stream)
+    _source_arg(what, src)
+    rows, cols = src.shape
+    outer, k = (rows, cols) if block_axis == 1 else (cols, rows)
+    if block_axis == 1:
+        _readable(what, "src", src, rows, cols)
+    if codes is None:
+        codes = codes_buffer(outer, k, src.device)
+    else:
+        _matrix(what, "codes", codes, outer, k, (torch.int8,))
+    if scales is None:
+        scales = torch.empty((outer,), dtype=torch.float32, device=src.device)
+    else:
+        _vector(what, "scales", scales, outer)
+    if mul is not None:
+        _vector(what, "mul", mul, k)
+    L = lib()
+    need = 0 if block_axis == 1 else _bytes(what, L.cfint8_quantize_workspace_bytes, rows, cols, block_axis)
+    wp, wb, held = _scratch(what, workspace, need, src.device, stream)
+    st = L.cfint8_quantize(src.data_ptr(), DTYPES[src.dtype], rows, cols, _ld(src, rows, cols), block_axis, _ptr(mul),
+                           codes.data_ptr(), _ld(codes, outer, k), scales.data_ptr(), wp, wb, _stream(stream))
+    _check(st, what)
+    return codes, scales
+
+
+def cfint8_dequantize(codes: torch.Tensor, scales: torch.Tensor, outer: int, k: int, dtype=torch.float32,
+                      dst: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """codes * scales, a scale for each row, as fp32 or bf16 (dst's dtype when it is given)."""
+    what = "cfint8_dequantize"
+    ts = [("codes", codes), ("scales", scales)]
+    _on_gpu(what, ts if dst is None else ts + [("dst", dst)], stream)
+    _codes(what, "codes", codes, outer, k)
+    _vector(what, "scales", scales, outer)
+    if dst is None:
+        if dtype not in DTYPES:
+            raise ValueError(f"{what}: dtype must be one of {tuple(DTYPES)}, got {dtype}")
+        per = 16 // dtype.itemsize
+        dst = torch.empty((outer, -(-k // per) * per), dtype=dtype, device=codes.device)[:, :k]
+    _matrix(what, "dst", dst, outer, k, tuple(DTYPES))
+    st = lib().cfint8_dequantize(codes.data_ptr(), _ld(codes, outer, k), scales.data_ptr(), outer, k,
+                                 dst.data_ptr(), DTYPES[dst.dtype], _ld(dst, outer, k), _stream(stream))
+    _check(st, what)
+    return dst
+
+
+def cfint8_gemm_workspace_bytes(M: int, N: int, K: int, trans_b: int = 0) -> int:
+    return _bytes("cfint8_gemm_workspace_bytes", lib().cfint8_gemm_workspace_bytes, M, N, K, trans_b)
+
+
+def cfint8_gemm(a: torch.Tensor, a_scales: Optional[torch.Tensor], b: torch.Tensor,
+                b_scales: Optional[torch.Tensor], M: int, N: int, K: int, trans_b: int = 0,
+                bias: Optional[torch.Tensor] = None, dtype=torch.float32, c: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """C[M, N] = (a . b^T) a_scales[:, None] b_scales + bias in fp32 or bf16 (c's dtype when it is given).
+    a: codes [M, K]; b: codes [N, K], or [K, N] with trans_b=1; scales of None are 1."""
+    what = "cfint8_gemm"
+    ts = [("a", a), ("b", b)]
+    for name, t in (("a_scales", a_scales), ("b_scales", b_scales), ("bias", bias), ("c", c),
+                    ("workspace", workspace)):
+        if t is not None:
+            ts.append((name, t))
+    _on_gpu(what, ts, stream)
+    _codes(what, "a", a, M, K)
+    if trans_b:
+        _codes(what, "b", b, K, N)
+    else:
+        _codes(what, "b", b, N, K)
+    if a_scales is not None:
+        _vector(what, "a_scales", a_scales, M)
+    if b_scales is not None:
+        _vector(what, "b_scales", b_scales, N)
+    if bias is not None:
+        _vector(what, "bias", bias, N)
+    if c is None:
+        if dtype not in DTYPES:
+            raise ValueError(f"{what}: dtype must be one of {tuple(DTYPES)}, got {dtype}")
+        c = torch.empty((M, N), dtype=dtype, device=a.device)
+    else:
+        _matrix(what, "c", c, M, N, tuple(DTYPES))
+    L = lib()
+    wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_gemm_workspace_bytes, M, N, K, trans_b), a.device,
+                            stream)
+    ldb = _ld(b, K, N) if trans_b else _ld(b, N, K)
+    st = L.cfint8_gemm(a.data_ptr(), _ld(a, M, K), _ptr(a_scales), b.data_ptr(), ldb, trans_b, _ptr(b_scales),
+                       _ptr(bias), M, N, K, c.data_ptr(), DTYPES[c.dtype], c.stride(0) if M > 1 else N, wp, wb,
+                       _stream(stream))
+    _check(st, what)
+    return c
+
+
+def cfint8_moe_workspace_bytes(T: int, E: int, topk: int, H: int, I: int) -> int:
+    return _bytes("cfint8_moe_workspace_bytes", lib().cfint8_moe_workspace_bytes, T, E, topk, H, I)
+
+
+def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gate_up_scales: torch.Tensor,
+               down: torch.Tensor, down_scales: torch.Tensor, topk: int, renormalize: bool = True,
+               active: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+               ids: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, stream=None):
+    """A mixture-of-experts layer on x [T, H] (fp32 or bf16): router [E, H] of x's dtype, gate_up codes
+    [E, 2 I, H] with scales [E, 2 I], down codes [E, H, I] with scales [E, H].  active: uint8 or bool
+    [T], 0 for padded tokens (zero rows, ids -1).  Returns y [T, H], ids int32 and weights fp32 [T, topk]."""
+    what = "cfint8_moe"
+    ts = [("x", x), ("router", router), ("gate_up", gate_up), ("gate_up_scales", gate_up_scales), ("down", down),
+          ("down_scales", down_scales)]
+    for name, t in (("active", active), ("y", y), ("ids", ids), ("weights", weights), ("workspace", workspace)):
+        if t is not None:
+            ts.append((name, t))
+    _on_gpu(what, ts, stream)
+    _source_arg(what, x)
+    T, H = x.shape
+    if router.dim() != 2 or router.shape[1] != H or router.dtype != x.dtype or not router.is_contiguous():
+        raise ValueError(f"{what}: router must be a contiguous [E, {H}] matrix of {x.dtype}, got "
+                         f"{tuple(router.shape)} {router.dtype}")
+    E = router.shape[0]
+    if down.dim() != 3 or down.shape[0] != E or down.shape[1] != H:
+        raise ValueError(f"{what}: down must be [{E}, {H}, I], got {tuple(down.shape)}")
+    I = down.shape[2]
+    if tuple(gate_up.shape) != (E, 2 * I, H):
+        raise ValueError(f"{what}: gate_up must be {(E, 2 * I, H)}, got {tuple(gate_up.shape)}")
+    for name, t in (("gate_up", gate_up), ("down", down)):
+        if t.dtype != torch.int8 or not t.is_contiguous():
+            raise ValueError(f"{what}: {name} must be contiguous torch.int8")
+    _vector(what, "gate_up_scales", gate_up_scales, E * 2 * I)
+    _vector(what, "down_scales", down_scales, E * H)
+    if active is not None:
+        _vector(what, "active", active, T, torch.bool if active.dtype == torch.bool else torch.uint8)
+    if y is None:
+        y = torch.empty((T, H), dtype=x.dtype, device=x.device)
+    else:
+        _matrix(what, "y", y, T, H, (x.dtype,))
+    if ids is None:
+        ids = torch.empty((T, topk), dtype=torch.int32, device=x.device)
+    else:
+        _vector(what, "ids", ids, T * topk, torch.int32)
+    if weights is None:
+        weights = torch.empty((T, topk), dtype=torch.float32, device=x.device)
+    else:
+        _vector(what, "weights", weights, T * topk)
+    L = lib()
+    wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_moe_workspace_bytes, T, E, topk, H, I), x.device,
+                            stream)
+    st = L.cfint8_moe(x.data_ptr(), DTYPES[x.dtype], T, H, _ld(x, T, H), router.data_ptr(), E, gate_up.data_ptr(),
+                      gate_up_scales.data_ptr(), down.data_ptr(), down_scales.data_ptr(), I, topk,
+                      1 if renormalize else 0, _ptr(active), y.data_ptr(), _ld(y, T, H), ids.data_ptr(),
+                      weights.data_ptr(), wp, wb, _stream(stream))
+    _check(st, what)
+    return y, ids, weights

@@ -1,0 +1,465 @@
+// 8-bit integer quantization with one fp32 scale for each line (a row, or a column through the
+// transpose), and its reconstruction.
+//
+//   s = fl32(max |v| / 127),  q = v / s rounded to nearest even, the quotient exact.
+//
+// The exact quotient matters: max / 2 lies within 2^-25 of 63.5 s in every line that holds it, on the side
+// that the rounding of s decides.  q0 = rint(v * fl32(1/s)) is within one of q, and v - q0 s is exact in one
+// fma (a multiple of half an ulp of s below s), so comparing it with s/2 settles q; that comparison
+// finds something to mend only next to a tie, and eight elements share it.
+//
+// Rows: held in registers by a wave (up to 2048) or a workgroup (up to 32768), the source read once; longer
+// ones read twice.  Columns: partial maxima of row chunks into the workspace (maxima, so no order to
+// depend on), then 128 x 128 tiles turned in LDS.  Bound by memory: the source and the codes.
+#include "device_util.hpp"
+#include "int8_internal.hpp"
+
+namespace cfint8 {
+
+using curvefp::Div32;
+using curvefp::div32;
+using curvefp::make_div32;
+
+namespace {
+
+constexpr uint32_t INF_BITS = 0x7F800000u;
+
+// what a line's elements are quantized with; pre = 2^64 for lines so small that 1 / s would overflow
+struct Line {
+    float s, inv, half, pre;
+    bool zero;   // zero codes: a line of zeros, or one that holds a NaN or an infinity
+    float out;   // the scale as stored
+};
+
+__device__ __forceinline__ Line make_line(uint32_t amax) {
+    Line l;
+    const float m = __uint_as_float(amax);
+    l.out = amax >= INF_BITS ? __uint_as_float(0x7FC00000u) : m / 127.0f;
+    l.zero = amax >= INF_BITS || l.out == 0.f;
+    l.pre = l.out < 0x1p-60f ? 0x1p64f : 1.f;
+    l.s = l.zero ? 1.f : l.out * l.pre;
+    l.inv = 1.f / l.s;
+    l.half = 0.5f * l.s;
+    return l;
+}
+
+// codes of 8 elements as two little-endian words
+__device__ __forceinline__ uint2 quant8(const float* v, const Line& l) {
+    float q[8], r[8], far = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float x = v[i] * l.pre;
+        q[i] = __builtin_rintf(x * l.inv);
+        r[i] = __builtin_fmaf(-q[i], l.s, x);
+        far = fmaxf(far, fabsf(r[i]));
+    }
+    if (far >= l.half) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float a = fabsf(r[i]);
+            const bool odd = ((int)q[i] & 1) != 0;
+            if (a > l.half || (a == l.half && odd)) q[i] += __builtin_copysignf(1.f, r[i]);
+        }
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        uint32_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) b[i] = (uint32_t)(int)__builtin_amdgcn_fmed3f(q[4 * h + i], -127.f, 127.f);
+        // byte 0 of each word, two at a time
+        const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000C0Cu);
+        w[h] = lo | hi;
+    }
+    if (l.zero) w[0] = w[1] = 0;
+    return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ void unpack_bf16(const uint4& u, float* v) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+
+// elements c .. c + 7 of a row of n at p, c a multiple of 8; zeros past its end.  ALIGNED: 16-byte aligned
+// rows.  BEHIND: read in pieces of 16 bytes, the last of which may reach behind the row's end
+template <bool BF16, bool ALIGNED, bool BEHIND, class I>
+__device__ __forceinline__ void load8(const char* p, I c, I n, float* v) {
+    if (ALIGNED && (BEHIND || c + 8 <= n)) {
+        const uint4* q = reinterpret_cast<const uint4*>(p + (int64_t)c * (BF16 ? 2 : 4));
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        if (BF16) {
+            unpack_bf16(c < n ? q[0] : none, v);
+        } else {
+            const uint4 a = c < n ? q[0] : none, b = c + 4 < n ? q[1] : none;
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = __uint_as_float(w[i]);
+        }
+        if (c + 8 > n) {
+#pragma unroll
+            for (int i = 1; i < 8; i++) v[i] = c + i < n ? v[i] : 0.f;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        v[i] = 0.f;
+        if (c + i < n) {
+            if (BF16) v[i] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(p)[c + i] << 16);
+            else v[i] = reinterpret_cast<const float*>(p)[c + i];
+        }
+    }
+}
+
+// times mul[c .. c + 7] (16-byte aligned), elements past the end left alone
+template <class I>
+__device__ __forceinline__ void mul8(const float* __restrict__ mul, I c, I n, float* v) {
+    if (c + 8 <= n) {
+        const float4 a = *reinterpret_cast<const float4*>(mul + c), b = *reinterpret_cast<const float4*>(mul + c + 4);
+        v[0] *= a.x, v[1] *= a.y, v[2] *= a.z, v[3] *= a.w;
+        v[4] *= b.x, v[5] *= b.y, v[6] *= b.z, v[7] *= b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; i++)
+            if (c + i < n) v[i] *= mul[c + i];
+    }
+}
+
+__device__ __forceinline__ uint32_t max8(uint32_t m, const float* v) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t m) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+    return m;
+}
+
+// codes c .. c + 7 of a row of n (c a multiple of 8); nothing behind the row's last
+template <class I>
+__device__ __forceinline__ void store8(int8_t* q, I c, I n, uint2 w) {
+    if (c + 8 <= n) {
+        *reinterpret_cast<uint2*>(q + c) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (c + i < n) q[c + i] = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+}
+
+// ---------------------------------------------------------------- rows
+
+// TPR threads hold a row of up to 8 TPR NU elements
+template <bool BF16, bool MUL, int TPR, int NU>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rows_kernel(
+    const char* __restrict__ src, int64_t rows, int cols, int64_t ld, const float* __restrict__ mul,
+    int8_t* __restrict__ codes, int64_t ldq, float* __restrict__ scales) {
+    constexpr int THREADS = TPR < 256 ? 256 : TPR, WAVES = TPR / 64;
+    __shared__ uint32_t red[WAVES > 1 ? WAVES : 1];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+    if (row >= rows) return;   // TPR = 64: whole waves, no barrier below
+    const char* p = src + row * ld * (BF16 ? 2 : 4);
+    float v[NU][8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int u = 0; u < NU; u++) load8<BF16, true, true>(p, (u * TPR + t) * 8, cols, v[u]);
+#pragma unroll
+    for (int u = 0; u < NU; u++) {
+        if (MUL) mul8(mul, (u * TPR + t) * 8, cols, v[u]);
+        m = max8(m, v[u]);
+    }
+    m = wave_max(m);
+    if (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) m = max(m, red[w]);
+    }
+    const Line l = make_line(m);
+    int8_t* q = codes + row * ldq;
+#pragma unroll
+    for (int u = 0; u < NU; u++) {
+        const int c = (u * TPR + t) * 8;
+        if (c < cols) store8(q, c, cols, quant8(v[u], l));
+    }
+    if (t == 0) scales[row] = l.out;
+}
+
+// rows past the register kernels' reach: the source is read twice
+template <bool BF16, bool MUL>
+__global__ __launch_bounds__(1024) void long_rows_kernel(const char* __restrict__ src, int64_t cols, int64_t ld,
+                                                         const float* __restrict__ mul, int8_t* __restrict__ codes,
+                                                         int64_t ldq, float* __restrict__ scales) {
+    __shared__ uint32_t red[16];
+    const int64_t row = blockIdx.x;
+    const char* p = src + row * ld * (BF16 ? 2 : 4);
+    float v[8];
+    uint32_t m = 0;
+    for (int64_t c = (int64_t)threadIdx.x * 8; c < cols; c += 8192) {
+        load8<BF16, true, true>(p, c, cols, v);
+        if (MUL) mul8(mul, c, cols, v);
+        m = max8(m, v);
+    }
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    for (int w = 0; w < 16; w++) m = max(m, red[w]);
+    const Line l = make_line(m);
+    for (int64_t c = (int64_t)threadIdx.x * 8; c < cols; c += 8192) {
+        load8<BF16, true, true>(p, c, cols, v);
+        if (MUL) mul8(mul, c, cols, v);
+        store8(codes + row * ldq, c, cols, quant8(v, l));
+    }
+    if (threadIdx.x == 0) scales[row] = l.out;
+}
+
+template <bool BF16, bool MUL>
+hipError_t launch_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* mul, int8_t* codes,
+                       int64_t ldq, float* scales, hipStream_t s) {
+    const char* p = static_cast<const char*>(src);
+    const dim3 wave_grid((unsigned)((rows + 3) / 4)), row_grid((unsigned)rows);
+#define CFINT8_ROWS(TPR, NU)                                                                                       \
+    rows_kernel<BF16, MUL, TPR, NU><<<TPR < 256 ? wave_grid : row_grid, TPR < 256 ? 256 : TPR, 0, s>>>(            \
+        p, rows, (int)cols, ld, mul, codes, ldq, scales)
+    if (cols <= 512) CFINT8_ROWS(64, 1);
+    else if (cols <= 1024) CFINT8_ROWS(64, 2);
+    else if (cols <= 2048) CFINT8_ROWS(256, 1);
+    else if (cols <= 4096) CFINT8_ROWS(256, 2);
+    else if constexpr (MUL) {   // the multiplier's values are held beside the row's: two units a thread
+        if (cols <= 8192) CFINT8_ROWS(512, 2);
+        else if (cols <= 16384) CFINT8_ROWS(1024, 2);
+        else long_rows_kernel<BF16, MUL><<<row_grid, 1024, 0, s>>>(p, cols, ld, mul, codes, ldq, scales);
+    } else {
+        if (cols <= 8192) CFINT8_ROWS(256, 4);
+        else if (cols <= 16384) CFINT8_ROWS(512, 4);
+        else if (cols <= 32768) CFINT8_ROWS(1024, 4);
+        else long_rows_kernel<BF16, MUL><<<row_grid, 1024, 0, s>>>(p, cols, ld, mul, codes, ldq, scales);
+    }
+#undef CFINT8_ROWS
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- columns
+
+constexpr int TILE = 128;         // columns and rows of a tile
+constexpr int MAX_CHUNKS = 32;    // row chunks with a partial maximum of their own
+
+int64_t col_chunks(int64_t rows) {
+    const int64_t n = (rows + 63) / 64;
+    return n < MAX_CHUNKS ? n : MAX_CHUNKS;
+}
+
+// partial[chunk][col] = largest |v| of the chunk's rows (fp32 bits)
+template <bool BF16, bool MUL, bool ALIGNED>
+__global__ __launch_bounds__(256) void col_max_kernel(const char* __restrict__ src, int64_t rows, int64_t cols,
+                                                      int64_t ld, const float* __restrict__ mul, int64_t chunk_rows,
+                                                      uint32_t* __restrict__ partial) {
+    __shared__ uint32_t red[16][TILE];
+    const int cl = threadIdx.x & 15, rl = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * TILE + cl * 8;
+    const int64_t r0 = (int64_t)blockIdx.y * chunk_rows, r1 = min(rows, r0 + chunk_rows);
+    uint32_t m[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) m[i] = 0;
+    if (c < cols)
+#pragma unroll 4
+        for (int64_t r = r0 + rl; r < r1; r += 16) {
+            float v[8];
+            load8<BF16, ALIGNED, false>(src + r * ld * (BF16 ? 2 : 4), c, cols, v);
+            const float f = MUL ? mul[r] : 1.f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) m[i] = max(m[i], __float_as_uint(MUL ? v[i] * f : v[i]) & 0x7FFFFFFFu);
+        }
+#pragma unroll
+    for (int i = 0; i < 8; i++) red[rl][cl * 8 + i] = m[i];
+    __syncthreads();
+    const int64_t col = (int64_t)blockIdx.x * TILE + threadIdx.x;
+    if (threadIdx.x < TILE && col < cols) {
+        uint32_t x = 0;
+#pragma unroll
+        for (int k = 0; k < 16; k++) x = max(x, red[k][threadIdx.x]);
+        partial[(int64_t)blockIdx.y * cols + col] = x;
+    }
+}
+
+// a tile of 128 rows x 128 columns: a thread quantizes 4 rows x 8 columns twice, words of 4 codes of one
+// column go to LDS (16-byte pieces of a column's 128 bytes XOR-swizzled by the column's group of 8, so that
+// the 16 lanes of a row segment spread over the banks), and leave as 16-byte pieces of code rows
+template <bool BF16, bool MUL, bool ALIGNED>
+__global__ __launch_bounds__(256) void cols_kernel(const char* __restrict__ src, int64_t rows, int64_t cols, int64_t ld,
+                                                   const float* __restrict__ mul, const uint32_t* __restrict__ partial,
+                                                   int chunks, int8_t* __restrict__ codes, int64_t ldq,
+                                                   float* __restrict__ scales) {
+    __shared__ uint32_t top[2][TILE];
+    __shared__ __attribute__((aligned(16))) uint32_t tile[TILE * TILE / 4];
+    const int tid = threadIdx.x;
+    const int64_t c0 = (int64_t)blockIdx.x * TILE, r0 = (int64_t)blockIdx.y * TILE;
+    {
+        const int64_t col = c0 + (tid & 127);
+        uint32_t m = 0;
+        if (col < cols)
+            for (int k = tid >> 7; k < chunks; k += 2) m = max(m, partial[(int64_t)k * cols + col]);
+        top[tid >> 7][tid & 127] = m;
+    }
+    const int cl = tid & 15, rl = tid >> 4;
+    const int64_t c = c0 + cl * 8;
+    float v[2][4][8];
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int64_t r = r0 + h * 64 + rl * 4 + i;
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[h][i][j] = 0.f;
+            if (r < rows && c < cols) {
+                load8<BF16, ALIGNED, false>(src + r * ld * (BF16 ? 2 : 4), c, cols, v[h][i]);
+                if (MUL) {
+                    const float f = mul[r];
+#pragma unroll
+                    for (int j = 0; j < 8; j++) v[h][i][j] *= f;
+                }
+            }
+        }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const Line l = make_line(max(top[0][cl * 8 + j], top[1][cl * 8 + j]));
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = v[i >> 2][i & 3][j];
+        const uint2 w = quant8(x, l);
+        // word of rows 4 rl .. (first half: piece rl / 4; second: 4 + rl / 4)
+        uint32_t* t = tile + (cl * 8 + j) * 32;
+        t[(((rl >> 2) ^ (cl & 7)) << 2) + (rl & 3)] = w.x;
+        t[(((4 + (rl >> 2)) ^ (cl & 7)) << 2) + (rl & 3)] = w.y;
+        if (blockIdx.y == 0 && rl == 0 && c + j < cols) scales[c + j] = l.out;
+    }
+    __syncthreads();
+    // 128 columns x 8 pieces of 16 codes
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int e = tid + k * 256, col = e >> 3, piece = e & 7;
+        const int64_t r = r0 + piece * 16;
+        if (c0 + col >= cols || r >= rows) continue;
+        const uint4 w = *reinterpret_cast<const uint4*>(tile + col * 32 + ((piece ^ ((col >> 3) & 7)) << 2));
+        int8_t* q = codes + (c0 + col) * ldq + r;
+        if (r + 16 <= rows) {
+            *reinterpret_cast<uint4*>(q) = w;
+        } else {
+            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                if (r + i < rows) q[i] = (int8_t)(x[i >> 2] >> (8 * (i & 3)));
+        }
+    }
+}
+
+template <bool BF16, bool MUL, bool ALIGNED>
+hipError_t launch_cols(const void* src, int64_t rows, int64_t cols, int64_t ld, const float* mul, int8_t* codes,
+                       int64_t ldq, float* scales, void* ws, hipStream_t s) {
+    const char* p = static_cast<const char*>(src);
+    uint32_t* partial = static_cast<uint32_t*>(ws);
+    const int64_t chunks = col_chunks(rows), chunk_rows = (rows + chunks - 1) / chunks;
+    const unsigned ct = (unsigned)((cols + TILE - 1) / TILE);
+    col_max_kernel<BF16, MUL, ALIGNED><<<dim3(ct, (unsigned)chunks), 256, 0, s>>>(p, rows, cols, ld, mul, chunk_rows,
+                                                                                partial);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    cols_kernel<BF16, MUL, ALIGNED><<<dim3(ct, (unsigned)((rows + TILE - 1) / TILE)), 256, 0, s>>>(
+        p, rows, cols, ld, mul, partial, (int)chunks, codes, ldq, scales);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- reconstruction
+
+// a workgroup takes `per` rows (short rows) or one segment of SEG elements of a row, four codes a thread
+constexpr int SEG = 4096;
+
+__device__ __forceinline__ uint32_t to_bf16(float f) {   // nearest even; NaN stays one
+    uint32_t u = __float_as_uint(f);
+    if ((u & 0x7FFFFFFFu) > INF_BITS) return 0x7FC0u;
+    u += 0x7FFFu + ((u >> 16) & 1u);
+    return u >> 16;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void dequantize_kernel(const int8_t* __restrict__ codes, int64_t ldq,
+                                                         const float* __restrict__ scales, int64_t outer, int64_t k,
+                                                         char* __restrict__ dst, int64_t ld, int per, Div32 dcols,
+                                                         int width) {
+    const int64_t row0 = (int64_t)blockIdx.x * per, c0 = (int64_t)blockIdx.y * SEG;
+    const int quads = (int)((min((int64_t)width, k - c0) + 3) >> 2);
+    const int total = quads * (int)min((int64_t)per, outer - row0);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < total; i += 256) {
+        const int r = per > 1 ? (int)div32((uint32_t)i, dcols) : 0;
+        const int64_t c = c0 + 4 * (int64_t)(i - r * quads), row = row0 + r;
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + row * ldq + c);
+        const float s = scales[row];
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) x[j] = (float)(int8_t)(w >> (8 * j)) * s;
+        char* d = dst + (row * ld + c) * (BF16 ? 2 : 4);
+        if (c + 4 <= k) {
+            if (BF16)
+                *reinterpret_cast<uint2*>(d) = make_uint2(to_bf16(x[0]) | to_bf16(x[1]) << 16,
+                                                          to_bf16(x[2]) | to_bf16(x[3]) << 16);
+            else
+                *reinterpret_cast<float4*>(d) = make_float4(x[0], x[1], x[2], x[3]);
+        } else {
+            for (int j = 0; j < 4; j++)
+                if (c + j < k) {
+                    if (BF16) reinterpret_cast<uint16_t*>(d)[j] = (uint16_t)to_bf16(x[j]);
+                    else reinterpret_cast<float*>(d)[j] = x[j];
+                }
+        }
+    }
+}
+
+}  // namespace
+
+int64_t quantize_workspace_bytes(int64_t rows, int64_t cols, int axis) {
+    return axis == 1 ? 0 : col_chunks(rows) * cols * 4;
+}
+
+hipError_t launch_quantize(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, int axis,
+                           const float* mul, int8_t* codes, int64_t ldq, float* scales, void* ws, hipStream_t s) {
+    const bool bf16 = dtype == 1;
+    if (axis == 1) {
+        if (bf16) return mul ? launch_rows<true, true>(src, rows, cols, ld, mul, codes, ldq, scales, s)
+                             : launch_rows<true, false>(src, rows, cols, ld, mul, codes, ldq, scales, s);
+        return mul ? launch_rows<false, true>(src, rows, cols, ld, mul, codes, ldq, scales, s)
+                   : launch_rows<false, false>(src, rows, cols, ld, mul, codes, ldq, scales, s);
+    }
+    const bool al = reinterpret_cast<uintptr_t>(src) % 16 == 0 && (ld * (bf16 ? 2 : 4)) % 16 == 0;
+#define CFINT8_COLS(B, M, A) launch_cols<B, M, A>(src, rows, cols, ld, mul, codes, ldq, scales, ws, s)
+    if (bf16) {
+        if (mul) return al ? CFINT8_COLS(true, true, true) : CFINT8_COLS(true, true, false);
+        return al ? CFINT8_COLS(true, false, true) : CFINT8_COLS(true, false, false);
+    }
+    if (mul) return al ? CFINT8_COLS(false, true, true) : CFINT8_COLS(false, true, false);
+    return al ? CFINT8_COLS(false, false, true) : CFINT8_COLS(false, false, false);
+#undef CFINT8_COLS
+}
+
+hipError_t launch_dequantize(const int8_t* codes, int64_t ldq, const float* scales, int64_t outer, int64_t k, void* dst,
+                             int dtype, int64_t ld, hipStream_t s) {
+    const int width = (int)(k < SEG ? k : SEG);
+    const int per = k >= SEG ? 1 : (int)(SEG / k > 64 ? 64 : SEG / k);
+    const dim3 grid((unsigned)((outer + per - 1) / per), (unsigned)((k + SEG - 1) / SEG));
+    const Div32 d = make_div32((uint32_t)((width + 3) / 4));
+    char* p = static_cast<char*>(dst);
+    if (dtype == 1) dequantize_kernel<true><<<grid, 256, 0, s>>>(codes, ldq, scales, outer, k, p, ld, per, d, width);
+    else dequantize_kernel<false><<<grid, 256, 0, s>>>(codes, ldq, scales, outer, k, p, ld, per, d, width);
+    return hipGetLastError();
+}
+
+}  // namespace cfint8
