@@ -72,8 +72,10 @@ __device__ __forceinline__ Tile tile_of(int b, int tiles_m, int tiles_n, int bm,
     t.valid = u < total && (b >> 3) < share;
     const int g = u / (GROUP * tiles_n), gh = min(GROUP, tiles_m - g * GROUP);
     const int local = u - g * GROUP * tiles_n;
-    t.m0 = (int64_t)(g * GROUP + local % gh) * bm;
-    t.n0 = (int64_t)(local / gh) * bn;
+    // the quotients are the same in all lanes but come from vector code: without this every use of them in a
+    // buffer descriptor would be a loop over the lanes' values
+    t.m0 = (int64_t)__builtin_amdgcn_readfirstlane(g * GROUP + local % gh) * bm;
+    t.n0 = (int64_t)__builtin_amdgcn_readfirstlane(local / gh) * bn;
     return t;
 }
 
