@@ -24,6 +24,22 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
+// a piece of 16 codes without those past the first `left`
+__device__ __forceinline__ i32x4 first_codes(i32x4 v, int left) {
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        const int b = left - 4 * w;   // codes of this word
+        v[w] = b >= 4 ? v[w] : b <= 0 ? 0 : (int)((uint32_t)v[w] & ((1u << (8 * b)) - 1));
+    }
+    return v;
+}
+
+// the piece at p, of which the line holds `left` codes: zeros past them
+__device__ __forceinline__ i32x4 load16(const int8_t* p, int left) {
+    const i32x4 zero = {0, 0, 0, 0};
+    return left > 0 ? first_codes(*reinterpret_cast<const i32x4*>(p), left) : zero;
+}
+
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -79,185 +95,212 @@ __device__ __forceinline__ Tile tile_of(int b, int tiles_m, int tiles_n, int bm,
     return t;
 }
 
+// LDS has 64 banks of 4 bytes and serves 16 lanes of a 16-byte read at a time, here the same piece of 16 rows: two
+// rows of 128 bytes cover the banks, so the rows of equal parity take eight places (row / 2), a row of 256 covers them,
+// so all sixteen take their own.  (With row % 8 for rows of 128 half of the LDS's cycles were conflicts.)
+template <int BK>
+__device__ __forceinline__ int swizzle(int row) { return BK == 128 ? (row >> 1) & 7 : row & 15; }
+
 constexpr int BK = 128;   // codes of a block
 
-// WT: MFMA tiles of 32 a wave takes along each side (4 or 2)
-template <int WT, bool BF16>
+// LDS has 64 banks of 4 bytes and serves 16 lanes of a 16-byte read at a time, here the same piece of 16 rows: two
+// rows of 128 bytes cover the banks, so the eight rows of equal parity take a place each.  (With row % 8 half of the
+// LDS's cycles were conflicts.)
+__device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
+
+// TM, TN: MFMA tiles of 32 that a wave takes along M and N; S: stages
+template <int TM, int TN, int S, bool BF16>
 __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int tiles_n) {
-    constexpr int BM = 64 * WT, WM = 32 * WT;
-    constexpr int HALF = BM * BK;                    // one operand's block
-    constexpr int COPIES = HALF / 4096;              // 1 KB copies of a wave for one operand's block
-    constexpr int MFMAS = WT * WT * 2, READS = WT * 4;   // of half a block
-    __shared__ __attribute__((aligned(16))) char st0[2 * HALF];
-    __shared__ __attribute__((aligned(16))) char st1[2 * HALF];
-    __shared__ __attribute__((aligned(16))) float vec[3][BM];
+    constexpr int BM = 64 * TM, BN = 64 * TN, WM = 32 * TM, WN = 32 * TN;
+    constexpr int PIECES = BK / 16, COPY_ROWS = 1024 / BK;      // of a row; of a 1 KB copy
+    constexpr int COPIES_A = BM * BK / 4096, COPIES_B = BN * BK / 4096;   // of a wave
+    constexpr int SLICES = BK / 64;                             // 32 codes each, of half a block
+    constexpr int MFMAS = TM * TN * SLICES, READS = (TM + TN) * SLICES;   // of half a block
+    static_assert(COPIES_A + COPIES_B == READS, "one copy goes with each read");
+    constexpr int HALF = BM * BK;                               // where a stage's B begins
+    constexpr int STAGE = HALF + BN * BK;
+    __shared__ __attribute__((aligned(16))) char st0[STAGE], st1[STAGE], st2[S > 2 ? STAGE : 16], st3[S > 3 ? STAGE : 16];
+    __shared__ __attribute__((aligned(16))) float vec_a[BM], vec_b[BN], vec_bias[BN];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Tile tile = tile_of((int)blockIdx.x, tiles_m, tiles_n, BM, BM);
+    const Tile tile = tile_of((int)blockIdx.x, tiles_m, tiles_n, BM, BN);
     if (!tile.valid) return;
     const int64_t m0 = tile.m0, n0 = tile.n0;
-    const int rows_a = (int)min((int64_t)BM, g.M - m0), rows_b = (int)min((int64_t)BM, g.N - n0);
+    const int rows_a = (int)min((int64_t)BM, g.M - m0), rows_b = (int)min((int64_t)BN, g.N - n0);
     const int K = (int)g.K, nkb = (K + BK - 1) / BK;
 
     bool any = false;
     if (tid < BM) {
-        const float sa = g.as && tid < rows_a ? g.as[m0 + tid] : 1.f, sb = g.bs && tid < rows_b ? g.bs[n0 + tid] : 1.f;
-        vec[0][tid] = sa;
-        vec[1][tid] = sb;
-        vec[2][tid] = g.bias && tid < rows_b ? g.bias[n0 + tid] : 0.f;
-        any = !moderate(sa) || !moderate(sb);
+        const float s = g.as && tid < rows_a ? g.as[m0 + tid] : 1.f;
+        vec_a[tid] = s;
+        any = !moderate(s);
+    }
+    if (tid < BN) {
+        const float s = g.bs && tid < rows_b ? g.bs[n0 + tid] : 1.f;
+        vec_b[tid] = s;
+        vec_bias[tid] = g.bias && tid < rows_b ? g.bias[n0 + tid] : 0.f;
+        any = any || !moderate(s);
     }
     any = __syncthreads_or(any);
 
-    // copies: lane l of a kilobyte brings row l / 8, piece (l % 8) ^ (row % 8); a row past the edge and a piece
-    // past K lie behind the descriptor's end and arrive as zeros
+    // copies: a lane brings 16 bytes of its row, the piece that belongs where it writes; a row past the edge and a
+    // piece past K lie behind the descriptor's end and arrive as zeros
     using lds_ptr = __attribute__((address_space(3))) void*;
-    const int piece = 16 * ((lane & 7) ^ (lane >> 3));
     const int8_t *A = g.a + m0 * g.lda, *B = g.b + n0 * g.ldb;
-    const int end_a = rows_a * (int)g.lda, end_b = rows_b * (int)g.ldb;
-    const int row0 = wave * COPIES * 8 + (lane >> 3);
-    const int offa = row0 * (int)g.lda, offb = row0 * (int)g.ldb;
-    auto copy = [&](int kb, char* st) {
-        const int k = kb * BK;
+    const int lda = (int)g.lda, ldb = (int)g.ldb, end_a = rows_a * lda, end_b = rows_b * ldb;
+    const int row_a = wave * COPIES_A * COPY_ROWS + lane / PIECES, row_b = wave * COPIES_B * COPY_ROWS + lane / PIECES;
+    auto piece = [&](int i, int left) __attribute__((always_inline)) {   // of copy i; a wave's rows start at a multiple of 16
+        const int p = 16 * ((lane % PIECES) ^ swizzle(i * COPY_ROWS + lane / PIECES));
+        return p < left ? p : 0x40000000;
+    };
+    // past the last block descriptors of no bytes, so that every step counts the same loads
+    auto copy = [&](int kb, char* st) __attribute__((always_inline)) {
+        const bool in = kb < nkb;
+        const int k = in ? kb * BK : 0;
         const __amdgpu_buffer_rsrc_t ra =
-            __builtin_amdgcn_make_buffer_rsrc((void*)(A + k), (short)0, end_a - k, 0x00020000);
+            __builtin_amdgcn_make_buffer_rsrc((void*)(A + k), (short)0, in ? end_a - k : 0, 0x00020000);
         const __amdgpu_buffer_rsrc_t rb =
-            __builtin_amdgcn_make_buffer_rsrc((void*)(B + k), (short)0, end_b - k, 0x00020000);
-        const int at = k + piece < K ? piece : 0x40000000;
+            __builtin_amdgcn_make_buffer_rsrc((void*)(B + k), (short)0, in ? end_b - k : 0, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < COPIES; i++) {
-            const int kbyte = (wave * COPIES + i) * 1024;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(st + kbyte), 16, offa + at + i * 8 * (int)g.lda, 0, 0,
-                                                     0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(st + HALF + kbyte), 16, offb + at + i * 8 * (int)g.ldb, 0,
+        for (int i = 0; i < COPIES_A; i++) {
+            const int at = row_a * lda + i * COPY_ROWS * lda + piece(i, K - k);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(st + (wave * COPIES_A + i) * 1024), 16, at, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < COPIES_B; i++) {
+            const int at = row_b * ldb + i * COPY_ROWS * ldb + piece(i, K - k);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(st + HALF + (wave * COPIES_B + i) * 1024), 16, at, 0,
                                                      0, 0);
         }
     };
-    // K ends inside a piece: A's codes behind it are cleared (B's then meet zeros)
-    auto clear_tail = [&](char* st) {
-        if (K % 16 == 0) return;
+    static_assert((COPIES_A * COPY_ROWS) % 16 == 0 && (COPIES_B * COPY_ROWS) % 16 == 0, "rows of a wave's copies");
+    // K ends inside a piece of block kb, the last: A's codes behind it are cleared (B's then meet zeros)
+    auto clear_tail = [&](int kb, char* st) __attribute__((always_inline)) {
+        if (kb != nkb - 1 || K % 16 == 0) return;
         if (tid < BM) {
             const int at = K % BK, p = at >> 4;
-            char* r = st + tid * BK + 16 * (p ^ (tid & 7));
+            char* r = st + tid * BK + 16 * (p ^ swizzle(tid));
             for (int i = at & 15; i < 16; i++) r[i] = 0;
         }
         __syncthreads();
     };
 
     const int wm = wave >> 1, wn = wave & 1, lr = lane & 31;
-    const int base_a = (wm * WM + lr) * BK, base_b = HALF + (wn * WM + lr) * BK;
+    const int base_a = (wm * WM + lr) * BK, base_b = HALF + (wn * WN + lr) * BK;
     struct Half {
-        i32x4 a[2][WT], b[2][WT];
+        i32x4 a[SLICES][TM], b[SLICES][TN];
     };
-    auto load_half = [&](Half& f, const char* st, int h) {
+    auto load_half = [&](Half& f, const char* st, int h) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < 2; s++) {
-            const int off = 16 * ((4 * h + 2 * s + (lane >> 5)) ^ (lr & 7));
+        for (int s = 0; s < SLICES; s++) {
+            const int off = 16 * ((2 * (h * SLICES + s) + (lane >> 5)) ^ swizzle(lr));
 #pragma unroll
-            for (int t = 0; t < WT; t++) f.a[s][t] = *reinterpret_cast<const i32x4*>(st + base_a + t * 32 * BK + off);
+            for (int t = 0; t < TM; t++) f.a[s][t] = *reinterpret_cast<const i32x4*>(st + base_a + t * 32 * BK + off);
 #pragma unroll
-            for (int t = 0; t < WT; t++) f.b[s][t] = *reinterpret_cast<const i32x4*>(st + base_b + t * 32 * BK + off);
+            for (int t = 0; t < TN; t++) f.b[s][t] = *reinterpret_cast<const i32x4*>(st + base_b + t * 32 * BK + off);
         }
     };
-    i32x16 acc[WT][WT] = {};
+    i32x16 acc[TM][TN] = {};
     // B is the row operand: a lane then holds four adjacent columns of one row of C
-    auto mfma = [&](const Half& f, int x) {
-        const int s = x / (WT * WT), i = (x / WT) % WT, j = (i & 1) ? WT - 1 - x % WT : x % WT;
+    auto mfma = [&](const Half& f, int x) __attribute__((always_inline)) {
+        const int s = x / (TM * TN), i = (x / TN) % TM, j = (i & 1) ? TN - 1 - x % TN : x % TN;
         acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.b[s][j], f.a[s][i], acc[i][j], 0, 0, 0);
     };
     constexpr int SG_MFMA = 0x008, SG_VMEM = 0x010, SG_DSR = 0x100;
-    constexpr int PER = MFMAS / READS > 0 ? MFMAS / READS : 1;   // MFMAS between two reads
-    auto phase1 = [&](Half& fa, Half& fb, char* st) {
+    // an even mix: GROUPS times (reads, copies, MFMAs)
+    constexpr int GROUPS = MFMAS < READS ? MFMAS : READS, RG = READS / GROUPS, MG = MFMAS / GROUPS;
+    auto phase1 = [&](Half& fa, Half& fb, char* st) __attribute__((always_inline)) {
         __builtin_amdgcn_s_waitcnt(0xC07F);   // fa's reads, a phase old
         load_half(fb, st, 1);
 #pragma unroll
         for (int x = 0; x < MFMAS; x++) mfma(fa, x);
 #pragma unroll
-        for (int i = 0; i < READS; i++) {
-            __builtin_amdgcn_sched_group_barrier(SG_DSR, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(SG_MFMA, PER, 0);
+        for (int i = 0; i < GROUPS; i++) {
+            __builtin_amdgcn_sched_group_barrier(SG_DSR, RG, 0);
+            __builtin_amdgcn_sched_group_barrier(SG_MFMA, MG, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto handover = [&] {
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's copies have landed
-        __syncthreads();
+    // every wave is done with its stage, and the next block has landed: only S - 2 newer ones are still out
+    // (vmcnt sits in bits 3:0 and 15:14, lgkmcnt in 11:8)
+    constexpr int OUT = (S - 2) * READS;
+    static_assert(OUT < 64, "vmcnt holds 6 bits");
+    auto handover = [&]() __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070 | (OUT & 15) | ((OUT >> 4) << 14));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto phase2 = [&](Half& fa, Half& fb, char* nx, bool more, int kb, char* st) {
-        if (more) copy(kb, st);
+    auto phase2 = [&](Half& fa, Half& fb, char* nx, int kb, char* st) __attribute__((always_inline)) {
+        copy(kb, st);
         load_half(fa, nx, 0);
 #pragma unroll
         for (int x = 0; x < MFMAS; x++) mfma(fb, x);
 #pragma unroll
-        for (int i = 0; i < READS; i++) {
-            __builtin_amdgcn_sched_group_barrier(SG_DSR, 1, 0);
-            if (more) __builtin_amdgcn_sched_group_barrier(SG_VMEM, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(SG_MFMA, PER, 0);
+        for (int i = 0; i < GROUPS; i++) {
+            __builtin_amdgcn_sched_group_barrier(SG_DSR, RG, 0);
+            __builtin_amdgcn_sched_group_barrier(SG_VMEM, RG, 0);
+            __builtin_amdgcn_sched_group_barrier(SG_MFMA, MG, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
     Half f0, f1;
-    auto step = [&](char* cur, char* nxt, int kb) {   // copies block kb into cur once done with it
+    auto step = [&](int kb, char* cur, char* nxt) __attribute__((always_inline)) {
         phase1(f0, f1, cur);
         handover();
-        phase2(f0, f1, nxt, true, kb, cur);
+        clear_tail(kb + 1, nxt);
+        phase2(f0, f1, nxt, kb + S, cur);
     };
-    auto step_before_last = [&](char* cur, char* nxt) {
-        phase1(f0, f1, cur);
-        handover();
-        clear_tail(nxt);
-        phase2(f0, f1, nxt, false, 0, cur);
-    };
-    auto step_last = [&](char* cur) {
-        phase1(f0, f1, cur);
+    // the last block always runs on the last stage: the first ones start behind stage 0 where S does not divide
+    char* const st[4] = {st0, st1, st2, st3};
+    const int odd = nkb % S;
+    auto begin = [&](auto from) __attribute__((always_inline)) {
+        constexpr int F = decltype(from)::value;   // the first block's stage
 #pragma unroll
-        for (int x = 0; x < MFMAS; x++) mfma(f1, x);
+        for (int d = 0; d < S; d++) copy(d, st[(F + d) % S]);
+        asm volatile("" ::: "memory");
+        constexpr int LEFT = (S - 1) * READS;
+        static_assert(LEFT < 64, "vmcnt holds 6 bits");
+        __builtin_amdgcn_s_waitcnt(0x0070 | (LEFT & 15) | ((LEFT >> 4) << 14));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        clear_tail(0, st[F]);
+        load_half(f0, st[F], 0);
+#pragma unroll
+        for (int d = F; d < S; d++)
+            if (F > 0) step(d - F, st[d], st[(d + 1) % S]);
     };
-    // the last two blocks always run on st0 then st1: with an odd number the first goes to st1
-    const bool odd = (nkb & 1) != 0;
-    char *first = odd ? st1 : st0, *second = odd ? st0 : st1;
-    copy(0, first);
-    handover();
-    if (nkb > 1) copy(1, second);
-    else clear_tail(first);
-    load_half(f0, first, 0);
-    if (nkb == 1) {
-        step_last(first);
-    } else {
-        int s = 0;
-        if (odd) {
-            step(st1, st0, 2);
-            s = 1;
-        }
-        for (; s + 3 < nkb; s += 2) {
-            step(st0, st1, s + 2);
-            step(st1, st0, s + 3);
-        }
-        step_before_last(st0, st1);
-        step_last(st1);
+    if (odd == 0) begin(std::integral_constant<int, 0>{});
+    else if (S == 2 || odd == 1) begin(std::integral_constant<int, S - 1>{});
+    else if (S == 3 || odd == 2) begin(std::integral_constant<int, S == 2 ? 1 : S - 2>{});
+    else begin(std::integral_constant<int, S == 4 ? 1 : S - 1>{});
+    for (int kb = odd; kb < nkb; kb += S) {
+#pragma unroll
+        for (int d = 0; d < S; d++) step(kb + d, st[d], st[(d + 1) % S]);
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);   // the copies of no bytes
 
     // Epilogue: 32 rows at a time through LDS of the wave's own, so that C is written in whole rows of the
     // wave's tile, 16 bytes a lane
     __syncthreads();   // every wave is done with the stages
-    constexpr int ES = BF16 ? 2 : 4, PITCH = WM * ES + 16, LANES = WM * ES / 16;   // lanes of a row
-    static_assert(2 * 32 * PITCH <= 2 * HALF, "two waves' rows fit a stage");
+    constexpr int ES = BF16 ? 2 : 4, PITCH = WN * ES + 16, LANES = WN * ES / 16;   // lanes of a row
+    static_assert(2 * 32 * PITCH <= STAGE, "two waves' rows fit a stage");
     char* mine = (wm ? st1 : st0) + wn * 32 * PITCH;
-    const int64_t mw = m0 + wm * WM, nw = n0 + wn * WM;
+    const int64_t mw = m0 + wm * WM, nw = n0 + wn * WN;
     char* C = static_cast<char*>(g.c) + (mw * g.ldc + nw) * ES;
     auto store = [&](auto mode) {
         constexpr bool ANY = decltype(mode)::value;
 #pragma unroll
-        for (int i = 0; i < WT; i++) {
-            const float sa = vec[0][wm * WM + 32 * i + lr];
+        for (int i = 0; i < TM; i++) {
+            const float sa = vec_a[wm * WM + 32 * i + lr];
 #pragma unroll
-            for (int j = 0; j < WT; j++)
+            for (int j = 0; j < TN; j++)
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
                     const int col = 32 * j + 8 * q + 4 * (lane >> 5);
-                    const float4 sb = *reinterpret_cast<const float4*>(&vec[1][wn * WM + col]);
-                    const float4 bi = *reinterpret_cast<const float4*>(&vec[2][wn * WM + col]);
+                    const float4 sb = *reinterpret_cast<const float4*>(&vec_b[wn * WN + col]);
+                    const float4 bi = *reinterpret_cast<const float4*>(&vec_bias[wn * WN + col]);
                     const float x = scaled<ANY>(acc[i][j][4 * q], sa, sb.x, bi.x);
                     const float y = scaled<ANY>(acc[i][j][4 * q + 1], sa, sb.y, bi.y);
                     const float z = scaled<ANY>(acc[i][j][4 * q + 2], sa, sb.z, bi.z);
@@ -288,6 +331,183 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
     };
     if (any) store(std::true_type{});
     else store(std::false_type{});
+}
+
+// ---------------------------------------------------------------- few rows
+
+// outputs m .. m + 3 of column n
+template <bool BF16>
+__device__ __forceinline__ void store_few(const GemmArgs& g, i32x4 s, int64_t m, int64_t n) {
+    if (n >= g.N) return;
+    const float sb = g.bs ? g.bs[n] : 1.f, bias = g.bias ? g.bias[n] : 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+        if (m + v >= g.M) break;
+        const float y = scaled_any(s[v], g.as ? g.as[m + v] : 1.f, sb, bias);
+        if (BF16) static_cast<uint16_t*>(g.c)[(m + v) * g.ldc + n] = (uint16_t)pack_bf16(y, y);
+        else static_cast<float*>(g.c)[(m + v) * g.ldc + n] = y;
+    }
+}
+
+// One or two tokens against a weight: bound by the weight's codes, which go from memory through registers to the
+// matrix cores.  A workgroup owns 16 columns, its waves take the K blocks of 64 in turn and add their sums in LDS.
+// Lane l of a fragment is line l % 16, codes 16 (l / 16) .. of a block, what the lane loads itself; BATCH blocks
+// are requested before the first is used.
+template <int WAVES, int BATCH, bool BF16>
+__global__ __launch_bounds__(64 * WAVES) void one_kernel(GemmArgs g) {
+    __shared__ __attribute__((aligned(16))) i32x4 red[WAVES][64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int K = (int)g.K, kq = 16 * (lane >> 4), whole = K / 64;   // blocks that no lane's piece leaves
+    const int row = lane & 15;
+    const bool live = row < g.M;
+    const int8_t* a = g.a + (live ? row : 0) * g.lda + kq;
+    const int8_t* b = g.b + min(n0 + row, g.N - 1) * g.ldb + kq;
+    const i32x4 zero = {0, 0, 0, 0};
+    i32x4 acc = zero;
+    int kb = wave;
+    for (; kb + (BATCH - 1) * WAVES < whole; kb += BATCH * WAVES) {
+        i32x4 fa[BATCH], fb[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; u++) {
+            const int k = (kb + u * WAVES) * 64;
+            fb[u] = *reinterpret_cast<const i32x4*>(b + k);
+            fa[u] = live ? *reinterpret_cast<const i32x4*>(a + k) : zero;
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; u++) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[u], fb[u], acc, 0, 0, 0);
+    }
+    for (; kb * 64 < K; kb += WAVES) {   // the rest, K's end among it
+        const int left = K - kb * 64 - kq;   // codes from this lane's piece on
+        const i32x4 fb = left > 0 ? *reinterpret_cast<const i32x4*>(b + kb * 64) : zero;
+        const i32x4 fa = live ? load16(a + kb * 64, left) : zero;
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa, fb, acc, 0, 0, 0);
+    }
+    red[wave][lane] = acc;
+    __syncthreads();
+    if (tid >= 64) return;
+    i32x4 s = red[0][tid];
+#pragma unroll
+    for (int w = 1; w < WAVES; w++) s += red[w][tid];
+    store_few<BF16>(g, s, 4 * (tid >> 4), n0 + (tid & 15));   // element v of lane l: row 4 (l / 16) + v, column l % 16
+}
+
+template <int WAVES, int BATCH>
+hipError_t launch_one(const GemmArgs& g, hipStream_t s) {
+    const unsigned grid = (unsigned)((g.N + 15) / 16);
+    if (g.c_bf16) one_kernel<WAVES, BATCH, true><<<grid, 64 * WAVES, 0, s>>>(g);
+    else one_kernel<WAVES, BATCH, false><<<grid, 64 * WAVES, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+// A few tokens against a weight: 16 MT x 16 NT outputs a workgroup, K shared out over its waves as above, operands
+// through LDS: direct loads of 16 lines a quarter of a wave cost the L1 a lookup for each, 64 a kilobyte (16 x 14336 x
+// 4096 waits on them: 19.7 us against 14.1), copies to LDS of whole 128-byte pieces of lines 16.  A wave copies its
+// own blocks of 128 codes into two slots of its own, so nothing waits for other waves until the sums meet; more slots
+// measured slower (fewer workgroups fit a unit).
+template <int MT, int NT, int WAVES, bool BF16>
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(GemmArgs g, int tiles_n) {
+    constexpr int TILE = 16 * 128, SLOT = (MT + NT) * TILE, COPIES = 2 * (MT + NT);
+    __shared__ __attribute__((aligned(16))) char ring0[WAVES * SLOT], ring1[WAVES * SLOT];
+    static_assert(MT * NT * 1024 <= SLOT, "a wave's sums fit its slot");
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tm = __builtin_amdgcn_readfirstlane((int)blockIdx.x / tiles_n), tn = (int)blockIdx.x - tm * tiles_n;
+    const int64_t m0 = (int64_t)tm * 16 * MT, n0 = (int64_t)tn * 16 * NT;
+    const int K = (int)g.K, nkb = (K + 127) / 128, mine = (nkb - wave + WAVES - 1) / WAVES;
+    using lds_ptr = __attribute__((address_space(3))) void*;
+    const int8_t *A = g.a + m0 * g.lda, *B = g.b + n0 * g.ldb;
+    const int lda = (int)g.lda, ldb = (int)g.ldb;
+    const int end_a = (int)min((int64_t)16 * MT, g.M - m0) * lda, end_b = (int)min((int64_t)16 * NT, g.N - n0) * ldb;
+    const int row_a = (lane >> 3) * lda, row_b = (lane >> 3) * ldb;
+    // this wave's j-th block; past its last one descriptors of no bytes, so that every step counts the same loads
+    auto copy = [&](int j, char* ring) {
+        const int k = (wave + j * WAVES) * 128;
+        const bool in = j < mine;
+        const __amdgpu_buffer_rsrc_t ra =
+            __builtin_amdgcn_make_buffer_rsrc((void*)(A + (in ? k : 0)), (short)0, in ? end_a - k : 0, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rb =
+            __builtin_amdgcn_make_buffer_rsrc((void*)(B + (in ? k : 0)), (short)0, in ? end_b - k : 0, 0x00020000);
+        int at[2];   // the piece that belongs where this lane writes, of even and of odd copies
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            at[i] = 16 * ((lane & 7) ^ swizzle(8 * i + (lane >> 3)));
+            at[i] = at[i] < K - k ? at[i] : 0x40000000;
+        }
+        char* st = ring + wave * SLOT;
+#pragma unroll
+        for (int i = 0; i < 2 * MT; i++) {
+            const int o = row_a + i * 8 * lda + at[i & 1];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(st + i * 1024), 16, o, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * NT; i++) {
+            const int o = row_b + i * 8 * ldb + at[i & 1];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(st + MT * TILE + i * 1024), 16, o, 0, 0, 0);
+        }
+    };
+    i32x4 acc[MT][NT] = {};
+    const int lr = lane & 15;
+    auto use = [&](int j, const char* ring) {
+        const char* st = ring + wave * SLOT;
+        const int kb = wave + j * WAVES;
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            const int piece = 4 * s + (lane >> 4), off = lr * 128 + 16 * (piece ^ swizzle(lr));
+            i32x4 fa[MT], fb[NT];
+#pragma unroll
+            for (int i = 0; i < MT; i++) fa[i] = *reinterpret_cast<const i32x4*>(st + i * TILE + off);
+#pragma unroll
+            for (int n = 0; n < NT; n++) fb[n] = *reinterpret_cast<const i32x4*>(st + (MT + n) * TILE + off);
+            if (kb == nkb - 1 && K % 16 != 0) {   // K ends inside a piece: A's codes behind it meet B's as zeros
+#pragma unroll
+                for (int i = 0; i < MT; i++) fa[i] = first_codes(fa[i], K - kb * 128 - 16 * piece);
+            }
+#pragma unroll
+            for (int i = 0; i < MT; i++)
+#pragma unroll
+                for (int n = 0; n < NT; n++)
+                    acc[i][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fb[n], acc[i][n], 0, 0, 0);
+        }
+    };
+    // a block has landed once only the next one's loads are out; s_waitcnt's vmcnt sits in bits 3:0 and 15:14
+    static_assert(COPIES < 64, "vmcnt holds 6 bits");
+    constexpr int WAIT = 0x0F70 | (COPIES & 15) | ((COPIES >> 4) << 14);
+    auto step = [&](int j, char* now, char* next) {   // next: the slot that the step before this one used
+        __builtin_amdgcn_s_waitcnt(0xC07F);           // its reads are done
+        copy(j + 1, next);
+        __builtin_amdgcn_s_waitcnt(WAIT);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        use(j, now);
+    };
+    copy(0, ring0);
+    for (int j = 0; j < mine; j += 2) {
+        step(j, ring0, ring1);
+        step(j + 1, ring1, ring0);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);   // no copy and no read is left in flight: the sums take the first slot
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int j = 0; j < NT; j++)
+            *reinterpret_cast<i32x4*>(ring0 + wave * SLOT + (i * NT + j) * 1024 + 16 * lane) = acc[i][j];
+    __syncthreads();
+    for (int e = tid; e < MT * NT * 64; e += 64 * WAVES) {
+        const int t = e >> 6, l = e & 63;
+        i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) s += *reinterpret_cast<const i32x4*>(ring0 + w * SLOT + 16 * e);
+        store_few<BF16>(g, s, m0 + 16 * (t / NT) + 4 * (l >> 4), n0 + 16 * (t % NT) + (l & 15));
+    }
+}
+
+template <int MT, int NT, int WAVES>
+hipError_t launch_few(const GemmArgs& g, hipStream_t s) {
+    const int64_t tm = (g.M + 16 * MT - 1) / (16 * MT), tn = (g.N + 16 * NT - 1) / (16 * NT);
+    if (g.c_bf16) few_kernel<MT, NT, WAVES, true><<<(unsigned)(tm * tn), 64 * WAVES, 0, s>>>(g, (int)tn);
+    else few_kernel<MT, NT, WAVES, false><<<(unsigned)(tm * tn), 64 * WAVES, 0, s>>>(g, (int)tn);
+    return hipGetLastError();
 }
 
 // ---------------------------------------------------------------- the operand of another product, read transposed
@@ -321,14 +541,45 @@ __global__ __launch_bounds__(256) void transpose_kernel(const int8_t* __restrict
 
 int64_t ceil_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
-template <int WT>
+template <int TM, int TN, int S>
 hipError_t launch_tiles(const GemmArgs& g, hipStream_t s) {
-    constexpr int BM = 64 * WT;
-    const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BM - 1) / BM;
+    const int64_t tm = (g.M + 64 * TM - 1) / (64 * TM), tn = (g.N + 64 * TN - 1) / (64 * TN);
     const unsigned grid = (unsigned)(((tm * tn + 7) / 8) * 8);
-    if (g.c_bf16) tile_kernel<WT, true><<<grid, 256, 0, s>>>(g, (int)tm, (int)tn);
-    else tile_kernel<WT, false><<<grid, 256, 0, s>>>(g, (int)tm, (int)tn);
+    if (g.c_bf16) tile_kernel<TM, TN, S, true><<<grid, 256, 0, s>>>(g, (int)tm, (int)tn);
+    else tile_kernel<TM, TN, S, false><<<grid, 256, 0, s>>>(g, (int)tm, (int)tn);
     return hipGetLastError();
+}
+
+// Route.  One or two rows against many columns load straight to registers: at least two workgroups for each unit cover
+// each other's waits (1 x 14336 x 4096 12.5 us against 13.2 through LDS; 1 x 4096 x 14336, one workgroup a unit, 14.9
+// against 12.0).  Up to 16 rows whose 16-column workgroups fit the units at once take these, eight waves where K gives
+// each at least two blocks (1 x 4096 x 14336 12.0 us against 15.9 with 32 x 32 tiles; 16 x 1024 x 1024 3.2 us against
+// 2.7 with four).  All else goes by the time of a tile's block of 128 codes and what a tile costs besides, as measured
+// with one tile on every unit (us; times with K = 4096: 256 x 256 67, 256 x 128 39, 128 x 128 23, 64 x 128 15.8,
+// 64 x 64 10.4, 32 x 32 6.6): the smaller tiles spend more on a product but fill the units with fewer rows.
+hipError_t launch_routed(const GemmArgs& g, hipStream_t s) {
+    auto tiles = [&](int64_t bm, int64_t bn) { return ((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
+    constexpr int64_t UNITS = 256;
+    if (g.M <= 2 && tiles(16, 16) >= 2 * UNITS) return launch_one<8, 8>(g, s);
+    if (g.M <= 16 && tiles(16, 16) <= UNITS)
+        return g.K >= 2048 ? launch_few<1, 1, 8>(g, s) : launch_few<1, 1, 4>(g, s);
+    const double blocks = (double)((g.K + 127) / 128);
+    auto cost = [&](int64_t bm, int64_t bn, double once, double tile, double block) {
+        return once + (double)((tiles(bm, bn) + UNITS - 1) / UNITS) * (tile + block * blocks);
+    };
+    const double c[6] = {cost(32, 32, 2.5, 0.3, 0.11),  cost(64, 64, 2.0, 0.5, 0.235), cost(64, 128, 2.5, 1.0, 0.345),
+                         cost(128, 128, 0.0, 4.0, 0.59), cost(256, 128, 0.0, 6.0, 1.02), cost(256, 256, 0.0, 8.0, 1.83)};
+    int best = 0;
+    for (int i = 1; i < 6; i++)
+        if (c[i] < c[best]) best = i;
+    switch (best) {
+        case 0: return launch_few<2, 2, 4>(g, s);
+        case 1: return launch_tiles<1, 1, 4>(g, s);
+        case 2: return launch_tiles<1, 2, 3>(g, s);
+        case 3: return launch_tiles<2, 2, 3>(g, s);
+        case 4: return launch_tiles<4, 2, 3>(g, s);
+        default: return launch_tiles<4, 4, 2>(g, s);
+    }
 }
 
 }  // namespace
@@ -346,8 +597,7 @@ hipError_t launch_gemm(const GemmArgs& args, hipStream_t s) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const int64_t big = ((g.M + 255) / 256) * ((g.N + 255) / 256);
-    return big >= 200 ? launch_tiles<4>(g, s) : launch_tiles<2>(g, s);
+    return launch_routed(g, s);
 }
 
 }  // namespace cfint8

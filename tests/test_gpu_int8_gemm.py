@@ -115,3 +115,30 @@ def test_outputs_past_32_bits():
     torch.cuda.synchronize()
     rows = [0, 1, 20000, 35791, 39999]
     R.same_bits(c[rows], R.gemm(a[rows], b, None, None, None, torch.bfloat16), "rows")
+
+
+# large enough for each tile shape: 64 x 64, 64 x 128, 128 x 128, 256 x 128, 256 x 256, with ends inside tiles, blocks of
+# 128 codes (one, two and three of them over) and pieces of 16; one and two rows against many columns, up to 16
+# rows against few
+@pytest.mark.parametrize("M,N,K", [
+    (1, 9001, 1100), (2, 8193, 333), (2, 16400, 4113), (16, 4090, 1000), (9, 4000, 2049), (16, 100, 5000),
+    (200, 4000, 1000), (250, 4090, 1001), (500, 4100, 1003), (1000, 4090, 900), (2040, 4090, 515), (2040, 4090, 641),
+    (4090, 4093, 129), (4090, 4093, 1037), (4096, 4096, 256)])
+def test_routes(M, N, K):
+    run(M, N, K, ld_extra=16)
+    run(M, N, K, dtype=torch.bfloat16, spread=30.0)        # scales that are not moderate
+
+
+def test_results_do_not_depend_on_the_route():
+    """The same rows and columns in products that take different kernels."""
+    K = 1537
+    rng = np.random.default_rng(8)
+    a, b = R.random_codes(rng, 4090, K), R.random_codes(rng, 4100, K)
+    sa, sb = np.exp(rng.standard_normal(4090)).astype(np.float32), np.exp(rng.standard_normal(4100)).astype(np.float32)
+    ta, tb, ga, gb = R.codes_tensor(a), R.codes_tensor(b), dev(sa), dev(sb)
+    whole = i8.cfint8_gemm(ta, ga, tb, gb, 4090, 4100, K)
+    for M, N in ((1, 4100), (2, 4100), (14, 3000), (40, 4100), (250, 4100), (512, 4100), (1024, 2100), (2048, 4100)):
+        say(f"[int8 gemm] route {M} x {N} x {K}")
+        c = i8.cfint8_gemm(ta, ga, tb, gb, M, N, K)
+        torch.cuda.synchronize()
+        R.same_bits(c, whole[:M, :N], f"{M} x {N}")
