@@ -94,8 +94,9 @@ int cfint8_gemm(const int8_t* a, int64_t lda, const float* a_scales, const int8_
  *   p[t][j] = exp(l_j - l_0) / sum over the topk slots (renormalize = 1) or over all experts (0);
  *   g = (x[t] . gate_up[e][i]) s, u = (x[t] . gate_up[e][I + i]) s, h[i] = g / (1 + exp(-g)) u;
  *   y[t] = sum_j p[t][j] (h . down[e_j]) s, rounded once to x's dtype.
- * Codes enter the products exactly; x (fp32) and h as 22 significant bits below the largest of their row;
- * accumulation is fp32 and its order depends on the sizes alone.
+ * Codes enter the products exactly.  x and h enter them in fixed point, 22 bits (dtype bf16) or 30 bits (fp32)
+ * below a power of two above the largest of a row of x or of 64 neighbours of h; the sums of up to 64 such
+ * products (all of a row's for x) are exact, their order in fp32 depends on the sizes alone.
  *   x        [T][ld_x] of `dtype` (fp32 or bf16), 16-byte aligned rows; T in [1, CFINT8_MOE_MAX_TOKENS].
  *   router   [E][H] of `dtype`, 16-byte aligned; E in [1, CFINT8_MOE_MAX_EXPERTS].
  *   gate_up  codes [E][2 I][H] (I gate rows, then I up rows), scales [E][2 I];
@@ -111,7 +112,7 @@ int cfint8_gemm(const int8_t* a, int64_t lda, const float* a_scales, const int8_
 #define CFINT8_MOE_MAX_TOKENS ((int64_t)256)
 #define CFINT8_MOE_MAX_EXPERTS ((int64_t)1024)
 #define CFINT8_MOE_MAX_TOPK ((int64_t)32)
-#define CFINT8_MOE_MAX_WIDTH ((int64_t)32768)
+#define CFINT8_MOE_MAX_WIDTH ((int64_t)16384)
 int64_t cfint8_moe_workspace_bytes(int64_t T, int64_t E, int64_t topk, int64_t H, int64_t I);
 int cfint8_moe(const void* x, int dtype, int64_t T, int64_t H, int64_t ld_x, const void* router, int64_t E,
                const int8_t* gate_up, const float* gate_up_scales, const int8_t* down, const float* down_scales,

@@ -6,12 +6,16 @@
 // 30 bits (fp32) below a power of two above its largest, split into 3 or 4 signed base-256 digits, one
 // product for each digit.  All sums of products are exact int32; the digits' sums meet in fp32.
 //
-//   router   logits in 64 bits (they decide, so they are right to the last bit), x into digits
-//   topk     a wave for each token: ids and weights
-//   gate_up  a workgroup for each (expert, 32 inner columns): h in fp32
-//   digits   h into digits
-//   down     a workgroup for each (expert, 64 output columns): weighted partial rows, one for each slot
-//   combine  a token's slots added in order
+//   router   logits in 64 bits (they decide, so they are right to the last bit); x into digits
+//   topk     a workgroup for each token: ids and weights (a few tokens: done by the next kernel's workgroups)
+//   gate_up  a workgroup for each (expert, 64 inner columns): h, as digits with a power of two for each 64 of a row
+//            (so that no workgroup waits for a whole row's largest value)
+//   down     a workgroup for each (expert, 128 output columns): weighted partial rows, one for each slot
+//   combine  a token's slots added in order (few slots: by the last of down's workgroups on a column slice)
+//
+// What one workgroup leaves for another of the same kernel is stored and loaded past the XCDs' own caches (agent
+// scope), each thread waits for its stores before the workgroup counts itself in, and the last one loads only then.
+#include "../../include/cfint8.h"
 #include "int8_internal.hpp"
 
 namespace cfint8 {
@@ -20,15 +24,21 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int POISON = INT32_MIN;      // exponent of a row that holds a NaN or an infinity
+constexpr int POISON = INT16_MIN;      // exponent of values among which is a NaN or an infinity
 constexpr int ROWS = 16;               // token rows of a matrix product
-constexpr int UP_COLS = 32;            // inner columns of a gate_up workgroup
-constexpr int DOWN_COLS = 64;          // output columns of a down workgroup
+constexpr int64_t UNITS = 256;         // compute units
+constexpr int RANKED = 2048;           // logits that gate_up ranks itself ..
+constexpr int RANKED_EXPERTS = 256;    // .. over at most so many experts
+constexpr int UP_COLS = 64;            // inner columns of a gate_up workgroup: h's columns of one exponent
+constexpr int DOWN_COLS = 128;         // output columns of a down workgroup
 
 // workspace
 struct Layout {
-    int64_t logits, xd, xe, h, hd, he, part, bytes;
+    int64_t logits, xd, xe, hd, he, part, counts, bytes;
 };
+
+// exponents of a row of h: one for each 64 columns, an even number
+__host__ __device__ constexpr int64_t exponents(int64_t I) { return (I + 2 * UP_COLS - 1) / (2 * UP_COLS) * 2; }
 
 Layout layout(int64_t T, int64_t E, int64_t topk, int64_t H, int64_t I) {
     Layout l;
@@ -42,10 +52,10 @@ Layout layout(int64_t T, int64_t E, int64_t topk, int64_t H, int64_t I) {
     l.logits = take(T * E * 4);
     l.xd = take(T * 4 * H);
     l.xe = take(T * 4);
-    l.h = take(S * I * 4);
     l.hd = take(S * 4 * I);
-    l.he = take(S * 4);
+    l.he = take(S * exponents(I) * 2);
     l.part = take(S * H * 4);
+    l.counts = take((H + DOWN_COLS - 1) / DOWN_COLS * 4);   // arrivals of down's workgroups on each column slice
     l.bytes = at;
     return l;
 }
@@ -85,15 +95,18 @@ __device__ __forceinline__ int digit_exponent(uint32_t m) {
     return __builtin_amdgcn_frexp_expf(__uint_as_float(m)) - (P == 4 ? 30 : 22);
 }
 
+// signed digits of a value, digit p in byte p
+__device__ __forceinline__ uint32_t digits_of(float v, int e) {
+    const int n = e == POISON ? 0 : (int)__builtin_rintf(__builtin_amdgcn_ldexpf(v, -e));
+    return ((uint32_t)n + 0x00808080u) ^ 0x00808080u;
+}
+
 // digits of 8 values, byte i of out[p] digit p of value i
 template <int P>
 __device__ __forceinline__ void digits8(const float* v, int e, uint2* out) {
     uint32_t q[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const int n = e == POISON ? 0 : (int)__builtin_rintf(__builtin_amdgcn_ldexpf(v[i], -e));
-        q[i] = ((uint32_t)n + 0x00808080u) ^ 0x00808080u;   // signed digits
-    }
+    for (int i = 0; i < 8; i++) q[i] = digits_of(v[i], e);
 #pragma unroll
     for (int p = 0; p < P; p++) {
         uint32_t w[2] = {0, 0};
@@ -103,62 +116,72 @@ __device__ __forceinline__ void digits8(const float* v, int e, uint2* out) {
     }
 }
 
-__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* red) {   // 256 threads
+__device__ __forceinline__ uint32_t wave_max(uint32_t m) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    return max(max(red[0], red[1]), max(red[2], red[3]));
+    return m;
 }
 
-// one row of n (a multiple of 16) values into digits [P][n]
-template <bool BF16, int P>
-__device__ __forceinline__ void row_digits(const char* src, int n, int8_t* dst, int* exponent, uint32_t* red) {
-    uint32_t m = 0;
-    for (int c = threadIdx.x * 8; c < n; c += 2048) {
-        float v[8];
-        load8<BF16>(src, c, v);
+__device__ __forceinline__ uint32_t max8(uint32_t m, const float* v) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    }
-    const int e = digit_exponent<P>(block_max(m, red));
-    for (int c = threadIdx.x * 8; c < n; c += 2048) {
-        float v[8];
-        uint2 d[P];
-        load8<BF16>(src, c, v);
-        digits8<P>(v, e, d);
-#pragma unroll
-        for (int p = 0; p < P; p++) *reinterpret_cast<uint2*>(dst + (int64_t)p * n + c) = d[p];
-    }
-    if (threadIdx.x == 0) *exponent = e;
+    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
 }
 
-// workgroups [0, T): a token's x into digits; then (4 experts, one a wave) x (4 tokens)
+template <int P>
+__device__ __forceinline__ void put_digits(const float* v, int e, int8_t* dst, int n, int c) {
+    uint2 d[P];
+    digits8<P>(v, e, d);
+#pragma unroll
+    for (int p = 0; p < P; p++) *reinterpret_cast<uint2*>(dst + (int64_t)p * n + c) = d[p];
+}
+
+// workgroups [0, T): a token's x into digits (the first one clears the arrival counts too); then one for each
+// (expert, 4 tokens), its waves sharing H
 template <bool BF16, int P>
 __global__ __launch_bounds__(256) void router_kernel(MoeArgs a, int8_t* __restrict__ xd, int* __restrict__ xe,
-                                                     float* __restrict__ logits) {
-    __shared__ uint32_t red[4];
-    const int T = (int)a.T, E = (int)a.E, H = (int)a.H;
+                                                     float* __restrict__ logits, int* __restrict__ counts, int ncounts) {
+    __shared__ uint32_t top[4];
+    __shared__ double part[4][4];
+    const int T = (int)a.T, E = (int)a.E, H = (int)a.H, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t es = BF16 ? 2 : 4;
     int b = blockIdx.x;
     if (b < T) {
-        row_digits<BF16, P>(static_cast<const char*>(a.x) + b * a.ldx * es, H, xd + (int64_t)b * P * H, xe + b, red);
+        if (b == 0)
+            for (int i = threadIdx.x; i < ncounts; i += 256) counts[i] = 0;
+        const char* src = static_cast<const char*>(a.x) + b * a.ldx * es;
+        int8_t* dst = xd + (int64_t)b * P * H;
+        uint32_t m = 0;
+        for (int c = threadIdx.x * 8; c < H; c += 2048) {
+            float v[8];
+            load8<BF16>(src, c, v);
+            m = max8(m, v);
+        }
+        m = wave_max(m);
+        if (lane == 0) top[wave] = m;
+        __syncthreads();
+        const int e = digit_exponent<P>(max(max(top[0], top[1]), max(top[2], top[3])));
+        for (int c = threadIdx.x * 8; c < H; c += 2048) {
+            float v[8];
+            load8<BF16>(src, c, v);
+            put_digits<P>(v, e, dst, H, c);
+        }
+        if (threadIdx.x == 0) xe[b] = e;
         return;
     }
     b -= T;
-    const int eg = (E + 3) / 4;
-    const int e = (b % eg) * 4 + (threadIdx.x >> 6), t0 = (b / eg) * 4, lane = threadIdx.x & 63;
-    if (e >= E) return;
+    const int e = b % E, t0 = (b / E) * 4, n = min(4, T - t0);
     double s[4] = {0, 0, 0, 0};
     const char* r = static_cast<const char*>(a.router) + (int64_t)e * H * es;
-    for (int c = lane * 8; c < H; c += 512) {
+    const char* x = static_cast<const char*>(a.x) + t0 * a.ldx * es;
+#pragma unroll 2
+    for (int c = threadIdx.x * 8; c < H; c += 2048) {
         float w[8];
         load8<BF16>(r, c, w);
 #pragma unroll
         for (int t = 0; t < 4; t++) {
-            if (t0 + t >= T) break;
             float v[8];
-            load8<BF16>(static_cast<const char*>(a.x) + (t0 + t) * a.ldx * es, c, v);
+            load8<BF16>(x + (t < n ? t : 0) * a.ldx * es, c, v);
 #pragma unroll
             for (int i = 0; i < 8; i++) s[t] = __builtin_fma((double)v[i], (double)w[i], s[t]);
         }
@@ -167,8 +190,11 @@ __global__ __launch_bounds__(256) void router_kernel(MoeArgs a, int8_t* __restri
     for (int t = 0; t < 4; t++) {
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s[t] += __shfl_xor(s[t], o);
-        if (lane == 0 && t0 + t < T) logits[(int64_t)(t0 + t) * E + e] = (float)s[t];
+        if (lane == 0) part[wave][t] = s[t];
     }
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t < n) logits[(int64_t)(t0 + t) * E + e] = (float)(((part[0][t] + part[1][t]) + part[2][t]) + part[3][t]);
 }
 
 // orders logits: NaN below everything, -0 as 0
@@ -178,243 +204,489 @@ __device__ __forceinline__ uint32_t order_key(float l) {
     return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// a wave for each token; lane l holds experts l, l + 64, ...
-__global__ __launch_bounds__(64) void topk_kernel(MoeArgs a, const float* __restrict__ logits) {
-    constexpr int MAX = (int)(1024 / 64);
-    const int t = blockIdx.x, lane = threadIdx.x, E = (int)a.E, k = (int)a.topk;
+// how many of a token's experts come before e: larger keys, and equal ones of lower index; keys has E of them, padded
+// with zeros to a multiple of 4
+__device__ __forceinline__ int rank_of(const uint32_t* keys, int E, int e) {
+    const uint32_t k = keys[e];
+    int r = 0;
+    for (int j = 0; j < E; j += 4) {
+        const uint4 q = *reinterpret_cast<const uint4*>(keys + j);
+        r += (q.x > k || (q.x == k && j < e)) + (q.y > k || (q.y == k && j + 1 < e)) +
+             (q.z > k || (q.z == k && j + 2 < e)) + (q.w > k || (q.w == k && j + 3 < e));
+    }
+    // the padding's zeros tie with NaN's key only, at indexes past every e
+    return r;
+}
+
+// ids and weights of token t by N threads (a multiple of 64), its logits' keys in LDS; red has N / 64 + 1 floats
+template <int N>
+__device__ __forceinline__ void take_topk(const MoeArgs& a, int t, const float* __restrict__ logits,
+                                          const uint32_t* keys, float* red) {
+    const int E = (int)a.E, k = (int)a.topk, tid = threadIdx.x;
     int32_t* ids = a.ids + (int64_t)t * k;
     float* weights = a.weights + (int64_t)t * k;
     if (a.active && !a.active[t]) {
-        for (int j = lane; j < k; j += 64) {
+        for (int j = tid; j < k; j += N) {
             ids[j] = -1;
             weights[j] = 0.f;
         }
         return;
     }
-    float l[MAX];
-    uint64_t key[MAX];
+    constexpr int PER = (1024 + N - 1) / N;
+    int rank[PER];
 #pragma unroll
-    for (int i = 0; i < MAX; i++) {
-        const int e = lane + 64 * i;
-        l[i] = e < E ? logits[(int64_t)t * E + e] : 0.f;
-        key[i] = e < E ? ((uint64_t)order_key(l[i]) << 32) | (0xFFFFFFFFu - (uint32_t)e) : 0;
+    for (int i = 0; i < PER; i++) {
+        const int e = tid + N * i;
+        rank[i] = e < E ? rank_of(keys, E, e) : 1024;
+        if (rank[i] == 0) red[0] = logits[(int64_t)t * E + e];
     }
-    float lead = 0.f, sum = 0.f, mine = 0.f;
-    int my_id = 0;
-    for (int j = 0; j < k; j++) {
-        uint64_t best = 0;
+    __syncthreads();
+    const float lead = red[0];
+    float sum = 0.f, w[PER];
 #pragma unroll
-        for (int i = 0; i < MAX; i++) best = max(best, key[i]);
+    for (int i = 0; i < PER; i++) {
+        const int e = tid + N * i;
+        w[i] = e < E ? expf(logits[(int64_t)t * E + e] - lead) : 0.f;
+        if (!a.renorm || rank[i] < k) sum += w[i];
+    }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, o));
-        const int e = (int)(0xFFFFFFFFu - (uint32_t)best);
-        float le = 0.f;
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if ((tid & 63) == 0) red[1 + (tid >> 6)] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int i = 0; i < N / 64; i++) sum += red[1 + i];
 #pragma unroll
-        for (int i = 0; i < MAX; i++)
-            if (key[i] == best) {
-                key[i] = 0;
-                le = l[i];
-            }
-        le = __shfl(le, e & 63);
-        if (j == 0) lead = le;
-        const float w = expf(le - lead);
-        sum += w;
-        if (lane == j) {
-            mine = w;
-            my_id = e;
+    for (int i = 0; i < PER; i++)
+        if (rank[i] < k) {
+            ids[rank[i]] = tid + N * i;
+            weights[rank[i]] = w[i] / sum;
+        }
+}
+
+__global__ __launch_bounds__(256) void topk_kernel(MoeArgs a, const float* __restrict__ logits) {
+    __shared__ __attribute__((aligned(16))) uint32_t keys[1024];
+    __shared__ float red[5];
+    const int t = blockIdx.x, E = (int)a.E;
+    for (int e = threadIdx.x; e < (E + 3) / 4 * 4; e += 256) keys[e] = e < E ? order_key(logits[(int64_t)t * E + e]) : 0;
+    __syncthreads();
+    take_topk<256>(a, t, logits, keys, red);
+}
+
+// An expert's slots, ascending (an expert is taken at most once by each token), found from ids by every wave for
+// itself: no barrier stands between a workgroup's start and its loads.  Returns their number
+__device__ __forceinline__ int find_rows(const int32_t* __restrict__ ids, int slots, int e, uint16_t* list) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int s0 = 0; s0 < slots; s0 += 512) {
+        int32_t id[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int s = s0 + 64 * i + lane;
+            id[i] = s < slots ? ids[s] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint64_t b = __ballot(id[i] == e);
+            if (id[i] == e) list[n + __popcll(b & ((1ull << lane) - 1))] = (uint16_t)(s0 + 64 * i + lane);
+            n += __popcll(b);
         }
     }
-    if (!a.renorm) {
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < MAX; i++) sum += lane + 64 * i < E ? expf(l[i] - lead) : 0.f;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    }
-    if (lane < k) {
-        ids[lane] = my_id;
-        weights[lane] = mine / sum;
-    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    return n;
 }
 
-// The slots (at most 8192) whose token takes expert e, ascending, in list[]; their number.  All threads
-struct Rows {
-    uint16_t list[256];   // an expert is taken at most once by each token
-    int n;
-};
-
-__device__ __forceinline__ void find_rows(const int32_t* __restrict__ ids, int slots, int e, Rows& r) {
-    __shared__ int cnt[4], base;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (threadIdx.x == 0) base = 0;
-    __syncthreads();
-    for (int s0 = 0; s0 < slots; s0 += 256) {
-        const int s = s0 + threadIdx.x;
-        const bool hit = s < slots && ids[s] == e;
-        const uint64_t b = __ballot(hit);
-        if (lane == 0) cnt[wave] = __popcll(b);
-        __syncthreads();
-        int at = base;
-        for (int w = 0; w < wave; w++) at += cnt[w];
-        if (hit) r.list[at + __popcll(b & ((1ull << lane) - 1))] = (uint16_t)s;
-        __syncthreads();
-        if (threadIdx.x == 0) base += cnt[0] + cnt[1] + cnt[2] + cnt[3];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) r.n = base;
-    __syncthreads();
-}
-
-// Which expert a workgroup's first index stands for: expert i itself where the experts are fewer than the
-// slots, else slot i's expert if no earlier slot has it too; -1 for none
+// Which expert a workgroup's first index i stands for: expert i itself where the experts are fewer than the
+// slots, else slot i's expert (its rows then begin with slot i, or another index has them); -1 for none
 __device__ __forceinline__ int expert_of(const int32_t* __restrict__ ids, int i, int slots, int E) {
     if (E <= slots) return i;
-    const int e = ids[i];
-    if (e < 0) return -1;
-    __shared__ int seen;
-    if (threadIdx.x == 0) seen = 0;
-    __syncthreads();
-    for (int s = threadIdx.x; s < i; s += 256)
-        if (ids[s] == e) seen = 1;
-    __syncthreads();
-    return seen ? -1 : e;
+    return ids[i];
 }
 
-// digit sums of 16 rows x 16 NT columns over this wave's share of K: lane l holds row (A) or column (B)
-// l % 16 at 16 (l / 16) of each 64; a[p] and b[t] point at this lane's line, live: its row exists
-template <int P, int NT>
-__device__ __forceinline__ void accumulate(const int8_t* a, int64_t plane, bool live, const int8_t* const (&b)[NT],
-                                           int K, i32x4 (&acc)[P][NT]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const i32x4 zero = {0, 0, 0, 0};
+// Both at once from the logits (at most RANKED): the expert that index i stands for, or -1, and its rows.  A wave
+// for each token counts the logits before the expert's
+template <int WAVES>
+__device__ __forceinline__ int rank_rows(const MoeArgs& a, const uint32_t* keys, int stride, int i, uint16_t* list,
+                                         int& n) {
+    __shared__ int count;
+    __shared__ int expert;
+    __shared__ int16_t rank[256];
+    const int T = (int)a.T, E = (int)a.E, k = (int)a.topk, tid = threadIdx.x, lane = tid & 63;
+    int e = i, first = T;   // tokens before `first` must not take e
+    if (E > T * k) {
+        first = i / k;
+        if (a.active && !a.active[first]) return -1;
+        if (tid < E && rank_of(keys + first * stride, E, tid) == i - first * k) expert = tid;
+        __syncthreads();
+        e = expert;
+    }
+    for (int t = tid >> 6; t < T; t += WAVES) {
+        const uint32_t* q = keys + t * stride;
+        const uint32_t key = q[e];
+        int before = 0;
+        for (int j = lane; j < E; j += 64) before += q[j] > key || (q[j] == key && j < e);
 #pragma unroll
-    for (int p = 0; p < P; p++)
+        for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
+        if (lane == 0) rank[t] = (int16_t)(before < k && (!a.active || a.active[t]) ? before : -1);
+    }
+    __syncthreads();
+    if (tid < 64) {
+        int found = 0;
+        for (int t0 = 0; t0 < T; t0 += 64) {
+            const int t = t0 + lane;
+            const bool hit = t < T && rank[t] >= 0;
+            const uint64_t b = __ballot(hit);
+            if (hit) list[found + __popcll(b & ((1ull << lane) - 1))] = (uint16_t)(t * k + rank[t]);
+            found += __popcll(b);
+        }
+        if (lane == 0) count = found;
+    }
+    __syncthreads();
+    n = count;
+    if (E > T * k && list[0] < first * k) return -1;   // an earlier token's workgroups have it
+    return e;
+}
+
+// this workgroup's arrival at a count that `all` workgroups reach: true in the last one.  Every thread's stores
+// have reached memory before the count does
+__device__ __forceinline__ bool last_of(int* count, int all) {
+    __shared__ int last;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+        last = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1;
+    __syncthreads();
+    return last != 0;
+}
+
+__device__ __forceinline__ void put(float* p, float v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float get(const float* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Products of 16 rows x 16 NT columns over one of SHARES shares of K, in blocks of 128; use(row digits' fragments,
+// codes' fragments, exponents) takes them half a block at a time.  Codes go through LDS: loads of
+// 16 lines a quarter of a wave cost the L1 a lookup for each, 64 a kilobyte, copies of whole 128-byte pieces of
+// lines 16.  A wave has two slots of its own and copies the next block while it uses this one; the few rows of
+// digits come straight to registers, a block ahead as well.
+constexpr int TILE = 16 * 128;   // bytes of a tile's block
+
+// line r's 16-byte pieces lie XOR-swizzled by r / 2: 16 lanes that read a piece of 16 lines then cover the 64 banks
+__device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
+
+// codes of up to 16 lines of K bytes, `lines` of them in the matrix
+struct Lines {
+    const int8_t* p;
+    int lines;
+};
+
+//
+// digits: row_offset is where this lane's row (l % 16) begins, or NONE.  EXPS: exponents too, one for each half block
+// of a row: exp_offset[v] is where those of row 4 (l / 16) + v begin, or NONE.
+constexpr int NONE = 0x40000000;   // past every buffer's end, and so is what is added to it: reads zeros
+
+template <int P, int NT, int SHARES, bool EXPS, class Use>
+__device__ __forceinline__ void stream(const int8_t* digits, int digits_bytes, int row_offset, const int16_t* exps,
+                                       int exps_bytes, const int (&exp_offset)[4], const Lines (&b)[NT], int K, int share,
+                                       char* ring0, char* ring1, Use use) {
+    constexpr int SLOT = NT * TILE, LOADS = 2 * NT + 2 * P + (EXPS ? 4 : 0);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15;
+    const int nkb = (K + 127) / 128, mine = (nkb - share + SHARES - 1) / SHARES;
+    using lds_ptr = __attribute__((address_space(3))) void*;
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)digits, (short)0, digits_bytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t re = __builtin_amdgcn_make_buffer_rsrc((void*)exps, (short)0, exps_bytes, 0x00020000);
+    i32x4 fa[2][2][P];
+    int fe[2][4];
+    // requests this wave's j-th block; every call issues LOADS loads, past the last block they read nothing
+    auto request = [&](int j, char* ring, i32x4 (&f)[2][P], int (&x)[4]) __attribute__((always_inline)) {
+        const int k = (share + j * SHARES) * 128;
+        const bool in = j < mine;
+        int at[2];   // the piece that belongs where this lane writes, of a tile's first and second eight lines
 #pragma unroll
-        for (int t = 0; t < NT; t++) acc[p][t] = zero;
-    for (int k0 = wave * 64; k0 < K; k0 += 256) {
-        const int k = k0 + 16 * (lane >> 4);
-        i32x4 fa[P], fb[NT];
+        for (int i = 0; i < 2; i++) {
+            at[i] = 16 * ((lane & 7) ^ swizzle(8 * i + (lane >> 3)));
+            at[i] = k + at[i] < K ? (8 * i + (lane >> 3)) * K + at[i] : NONE;
+        }
 #pragma unroll
-        for (int t = 0; t < NT; t++) fb[t] = k < K ? *reinterpret_cast<const i32x4*>(b[t] + k) : zero;
+        for (int t = 0; t < NT; t++) {
+            const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(b[t].p + (in ? k : 0)), (short)0, in ? max(b[t].lines * K - k, 0) : 0, 0x00020000);
 #pragma unroll
-        for (int p = 0; p < P; p++) fa[p] = live && k < K ? *reinterpret_cast<const i32x4*>(a + p * plane + k) : zero;
+            for (int i = 0; i < 2; i++)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(ring + wave * SLOT + t * TILE + i * 1024), 16,
+                                                         at[i], 0, 0, 0);
+        }
 #pragma unroll
-        for (int t = 0; t < NT; t++)
+        for (int s = 0; s < 2; s++) {
+            const int ks = k + 64 * s + 16 * (lane >> 4);
+            const int off = (ks < K ? row_offset : NONE) + ks;
 #pragma unroll
             for (int p = 0; p < P; p++)
-                acc[p][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[p], fb[t], acc[p][t], 0, 0, 0);
+                f[s][p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, off + p * K, 0, 0));
+        }
+        if (EXPS) {
+            const int at_k = in ? k / 32 : NONE / 2;
+#pragma unroll
+            for (int v = 0; v < 4; v++) x[v] = (int)__builtin_amdgcn_raw_buffer_load_b32(re, exp_offset[v] + at_k, 0, 0);
+        }
+    };
+    // a block has landed once only the next one's loads are out; s_waitcnt's vmcnt sits in bits 3:0 and 15:14
+    static_assert(LOADS < 64, "vmcnt holds 6 bits");
+    constexpr int WAIT = 0x0F70 | (LOADS & 15) | ((LOADS >> 4) << 14);
+    auto step = [&](int j, char* now, char* next, i32x4 (&f)[2][P], i32x4 (&g)[2][P], int (&x)[4],
+                    int (&y)[4]) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // the next slot's reads, a step old, are done
+        request(j + 1, next, g, y);
+        __builtin_amdgcn_s_waitcnt(WAIT);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            i32x4 fb[NT];
+            const char* st = now + wave * SLOT + lr * 128 + 16 * ((4 * s + (lane >> 4)) ^ swizzle(lr));
+#pragma unroll
+            for (int t = 0; t < NT; t++) fb[t] = *reinterpret_cast<const i32x4*>(st + t * TILE);
+            int ex[4];
+#pragma unroll
+            for (int v = 0; v < 4; v++) ex[v] = EXPS ? (s ? x[v] >> 16 : (int16_t)x[v]) : 0;
+            use(f[s], fb, ex);
+        }
+    };
+    request(0, ring0, fa[0], fe[0]);
+    for (int j = 0; j < mine; j += 2) {
+        step(j, ring0, ring1, fa[0], fa[1], fe[0], fe[1]);
+        step(j + 1, ring1, ring0, fa[1], fa[0], fe[1], fe[0]);
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);   // no copy and no read is left in flight: the sums take the first slot
 }
 
-// the waves' sums: red[wave][t][column l % 16][row]; the digits meet here
+// element v of a lane's sums with the digits joined
 template <int P, int NT>
-__device__ __forceinline__ void share(const i32x4 (&acc)[P][NT], float* red) {
+__device__ __forceinline__ float join(const i32x4 (&acc)[P][NT], int t, int v) {
+    float f = (float)acc[P - 1][t][v];
+#pragma unroll
+    for (int p = P - 2; p >= 0; p--) f = __builtin_fmaf(f, 256.f, (float)acc[p][t][v]);
+    return f;
+}
+
+// the waves' sums into their first slots: [t][lane], element v of lane l is row 4 (l / 16) + v of column l % 16
+template <int NT>
+__device__ __forceinline__ void share_sums(const float (&f)[NT][4], char* ring0) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int t = 0; t < NT; t++)
-#pragma unroll
-        for (int v = 0; v < 4; v++) {
-            float f = (float)acc[P - 1][t][v];
-#pragma unroll
-            for (int p = P - 2; p >= 0; p--) f = __builtin_fmaf(f, 256.f, (float)acc[p][t][v]);
-            red[((wave * NT + t) * 16 + (lane & 15)) * ROWS + 4 * (lane >> 4) + v] = f;
-        }
+        *reinterpret_cast<float4*>(ring0 + wave * NT * TILE + t * 1024 + 16 * lane) =
+            make_float4(f[t][0], f[t][1], f[t][2], f[t][3]);
     __syncthreads();
 }
 
-// NaN for a poisoned row
-__device__ __forceinline__ float row_scaled(float f, int e, float s) {
-    return e == POISON ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(f, e) * s;
+// rows 4 q .. 4 q + 3 of column c of tile t, over the waves that share these columns (every other one from `half`)
+template <int NT, int WAVES>
+__device__ __forceinline__ void shared_sum(const char* ring0, int half, int t, int q, int c, float (&out)[4]) {
+    const char* at = ring0 + t * 1024 + 16 * (16 * q + c);
+    float4 s = *reinterpret_cast<const float4*>(at + half * NT * TILE);
+#pragma unroll
+    for (int w = 2; w < WAVES; w += 2) {
+        const float4 v = *reinterpret_cast<const float4*>(at + (half + w) * NT * TILE);
+        s.x += v.x;
+        s.y += v.y;
+        s.z += v.z;
+        s.w += v.w;
+    }
+    out[0] = s.x, out[1] = s.y, out[2] = s.z, out[3] = s.w;
 }
 
-template <int P>
-__global__ __launch_bounds__(256) void gate_up_kernel(MoeArgs a, const int8_t* __restrict__ xd,
-                                                      const int* __restrict__ xe, float* __restrict__ h) {
-    constexpr int NT = 2 * UP_COLS / 16, HALF = NT / 2;
-    __shared__ Rows rows;
-    __shared__ __attribute__((aligned(16))) float red[4 * NT * 16 * ROWS];
-    const int slots = (int)(a.T * a.topk), H = (int)a.H, I = (int)a.I, lane = threadIdx.x & 63;
-    const int nsl = (I + UP_COLS - 1) / UP_COLS;
-    const int e = expert_of(a.ids, blockIdx.x / nsl, slots, (int)a.E);
-    if (e < 0) return;
-    find_rows(a.ids, slots, e, rows);
-    const int c0 = (blockIdx.x % nsl) * UP_COLS;
-    const int8_t* b[NT];
+// f 2^e; NaN where e says so
+__device__ __forceinline__ float scaled_by(float f, int e) {
+    return e == POISON ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(f, e);
+}
+__device__ __forceinline__ float row_scaled(float f, int e, float s) { return scaled_by(f, e) * s; }
+
+// FEW: the logits are ranked here.  Waves of even number take the first 32 columns, the others the last
+template <int P, int WAVES, bool FEW>
+__global__ __launch_bounds__(64 * WAVES, 2) void gate_up_kernel(MoeArgs a, const int8_t* __restrict__ xd,
+                                                             const int* __restrict__ xe,
+                                                             const float* __restrict__ logits,
+                                                             int8_t* __restrict__ hd, int16_t* __restrict__ he,
+                                                             int experts) {
+    constexpr int NT = 4, THREADS = 64 * WAVES;   // tiles: 2 of gate, 2 of up
+    __shared__ uint16_t lists[FEW ? 1 : WAVES][256];
+    __shared__ __attribute__((aligned(16))) char ring0[WAVES * NT * TILE], ring1[WAVES * NT * TILE];
+    const int T = (int)a.T, E = (int)a.E, k = (int)a.topk, slots = T * k, H = (int)a.H, I = (int)a.I;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nsl = (I + UP_COLS - 1) / UP_COLS, index = (int)blockIdx.x / nsl;
+    uint16_t* rows = lists[FEW ? 0 : wave];
+    int e, n = 0;
+    if (FEW) {
+        __shared__ __attribute__((aligned(16))) uint32_t keys[RANKED + 4 * 256];
+        __shared__ float sums[WAVES + 1];
+        const int stride = (E + 3) / 4 * 4;
+        for (int i = threadIdx.x; i < T * stride; i += THREADS) {
+            const int t = i / stride, j = i - t * stride;
+            keys[i] = j < E ? order_key(logits[t * E + j]) : 0;
+        }
+        __syncthreads();
+        if (index >= experts) {   // the last T workgroups: a token's ids and weights for everyone else
+            const int t = (int)blockIdx.x - experts * nsl;
+            take_topk<THREADS>(a, t, logits, keys + t * stride, sums);
+            return;
+        }
+        e = rank_rows<WAVES>(a, keys, stride, index, rows, n);
+        if (e < 0 || n == 0) return;
+    } else {
+        e = expert_of(a.ids, index, slots, E);
+        if (e < 0) return;
+        n = find_rows(a.ids, slots, e, rows);
+        if (n == 0 || (E > slots && rows[0] != index)) return;
+    }
+    const int slice = (int)blockIdx.x % nsl, c0 = slice * UP_COLS, half = wave & 1;
+    Lines b[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
-        const int c = min(c0 + 16 * (t % HALF) + (lane & 15), I - 1) + (t >= HALF ? I : 0);
-        b[t] = a.gu + ((int64_t)e * 2 * I + c) * H;
+        const int c = c0 + 32 * half + 16 * (t & 1);   // columns come in sixteens: a tile is there or not
+        b[t].lines = c < I ? 16 : 0;
+        b[t].p = a.gu + ((int64_t)__builtin_amdgcn_readfirstlane(e) * 2 * I + c + (t >= 2 ? I : 0)) * H;
     }
-    for (int r0 = 0; r0 < rows.n; r0 += ROWS) {
+    for (int r0 = 0; r0 < n; r0 += ROWS) {
         const int r = r0 + (lane & 15);
-        const bool live = r < rows.n;
-        const int8_t* x = xd + (int64_t)(live ? rows.list[r] / (int)a.topk : 0) * P * H;
-        i32x4 acc[P][NT];
-        accumulate<P, NT>(x, H, live, b, H, acc);
-        share<P, NT>(acc, red);
-        for (int i = threadIdx.x; i < UP_COLS * ROWS; i += 256) {
-            const int row = i / UP_COLS, col = i % UP_COLS;
-            if (r0 + row >= rows.n || c0 + col >= I) continue;
-            const int at = ((col >> 4) * 16 + (col & 15)) * ROWS + row;
-            float g = 0.f, u = 0.f;
+        i32x4 acc[P][NT] = {};
+        const int none[4] = {NONE, NONE, NONE, NONE};
+        stream<P, NT, WAVES / 2, false>(
+            xd, T * P * H, r < n ? rows[r] / k * P * H : NONE, nullptr, 0, none, b, H, wave >> 1, ring0, ring1,
+            [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&)[4]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int w = 0; w < 4; w++) {
-                g += red[w * NT * 16 * ROWS + at];
-                u += red[(w * NT + HALF) * 16 * ROWS + at];
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int p = 0; p < P; p++)
+                        acc[p][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[p], fb[t], acc[p][t], 0, 0, 0);
+            });
+        float f[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; t++)
+#pragma unroll
+            for (int v = 0; v < 4; v++) f[t][v] = join<P, NT>(acc, t, v);
+        share_sums<NT>(f, ring0);
+        // a wave for each four rows, a lane for each column
+        const int c = c0 + lane, q = wave;
+        if (q < 4 && r0 + 4 * q < n) {
+            float g[4], u[4], sg = 0.f, su = 0.f;
+            shared_sum<NT, WAVES>(ring0, lane >> 5, (lane >> 4) & 1, q, lane & 15, g);
+            shared_sum<NT, WAVES>(ring0, lane >> 5, 2 + ((lane >> 4) & 1), q, lane & 15, u);
+            if (c < I) {
+                const float* s = a.gus + (int64_t)e * 2 * I + c;
+                sg = s[0], su = s[I];
             }
-            const int slot = rows.list[r0 + row], ex = xe[slot / (int)a.topk];
-            const float* s = a.gus + (int64_t)e * 2 * I + c0 + col;
-            g = row_scaled(g, ex, s[0]);
-            u = row_scaled(u, ex, s[I]);
-            h[(int64_t)slot * I + c0 + col] = g / (1.f + expf(-g)) * u;
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                if (r0 + 4 * q + v >= n) break;
+                const int slot = rows[r0 + 4 * q + v], ex = xe[slot / k];
+                const float gv = row_scaled(g[v], ex, sg), uv = row_scaled(u[v], ex, su);
+                const float y = c < I ? gv / (1.f + expf(-gv)) * uv : 0.f;
+                const int eh = digit_exponent<P>(wave_max(__float_as_uint(y) & 0x7FFFFFFFu));
+                const uint32_t d = digits_of(y, eh);
+                int8_t* dst = hd + (int64_t)slot * P * I + c;
+                if (c < I)
+#pragma unroll
+                    for (int p = 0; p < P; p++) dst[(int64_t)p * I] = (int8_t)(d >> (8 * p));
+                if (lane == 0) he[slot * exponents(I) + slice] = (int16_t)eh;
+            }
         }
         __syncthreads();
     }
 }
 
-template <int P>
-__global__ __launch_bounds__(256) void digits_kernel(MoeArgs a, const float* __restrict__ h, int8_t* __restrict__ hd,
-                                                     int* __restrict__ he) {
-    __shared__ uint32_t red[4];
-    const int slot = blockIdx.x;
-    if (a.ids[slot] < 0) return;
-    row_digits<false, P>(reinterpret_cast<const char*>(h + (int64_t)slot * a.I), (int)a.I, hd + (int64_t)slot * P * a.I,
-                         he + slot, red);
+template <bool BF16>
+__device__ __forceinline__ void store4(const MoeArgs& a, int t, int c, const float4& s) {
+    char* y = static_cast<char*>(a.y) + (t * a.ldy + c) * (BF16 ? 2 : 4);
+    if (BF16) *reinterpret_cast<uint2*>(y) = make_uint2(to_bf16(s.x) | to_bf16(s.y) << 16, to_bf16(s.z) | to_bf16(s.w) << 16);
+    else *reinterpret_cast<float4*>(y) = s;
 }
 
-template <int P>
-__global__ __launch_bounds__(256) void down_kernel(MoeArgs a, const int8_t* __restrict__ hd, const int* __restrict__ he,
-                                                   float* __restrict__ part) {
-    constexpr int NT = DOWN_COLS / 16;
-    __shared__ Rows rows;
-    __shared__ __attribute__((aligned(16))) float red[4 * NT * 16 * ROWS];
-    const int slots = (int)(a.T * a.topk), H = (int)a.H, I = (int)a.I, lane = threadIdx.x & 63;
-    const int nsl = (H + DOWN_COLS - 1) / DOWN_COLS;
-    const int e = expert_of(a.ids, blockIdx.x / nsl, slots, (int)a.E);
-    if (e < 0) return;
-    find_rows(a.ids, slots, e, rows);
-    const int c0 = (blockIdx.x % nsl) * DOWN_COLS;
-    const int8_t* b[NT];
+// FEW: the last workgroup of a column slice adds the slots
+template <int P, int WAVES, bool FEW, bool BF16>
+__global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const int8_t* __restrict__ hd,
+                                                          const int16_t* __restrict__ he, float* part, int* counts,
+                                                          int experts) {
+    constexpr int NT = DOWN_COLS / 32, THREADS = 64 * WAVES;
+    __shared__ uint16_t lists[WAVES][256];
+    __shared__ __attribute__((aligned(16))) char ring0[WAVES * NT * TILE], ring1[WAVES * NT * TILE];
+    const int k = (int)a.topk, slots = (int)a.T * k, H = (int)a.H, I = (int)a.I, E = (int)a.E;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave & 1;
+    const int nsl = (H + DOWN_COLS - 1) / DOWN_COLS, slice = (int)blockIdx.x % nsl, c0 = slice * DOWN_COLS;
+    const int index = (int)blockIdx.x / nsl, e = expert_of(a.ids, index, slots, E), row_exps = (int)exponents(I);
+    uint16_t* rows = lists[wave];
+    int n = e >= 0 ? find_rows(a.ids, slots, e, rows) : 0;
+    if (n > 0 && E > slots && rows[0] != index) n = 0;
+    Lines b[NT];
 #pragma unroll
-    for (int t = 0; t < NT; t++) b[t] = a.dn + ((int64_t)e * H + min(c0 + 16 * t + (lane & 15), H - 1)) * I;
-    for (int r0 = 0; r0 < rows.n; r0 += ROWS) {
+    for (int t = 0; t < NT; t++) {
+        const int c = c0 + 64 * half + 16 * t;
+        b[t].lines = c < H ? 16 : 0;
+        b[t].p = a.dn + ((int64_t)__builtin_amdgcn_readfirstlane(max(e, 0)) * H + c) * I;
+    }
+    for (int r0 = 0; r0 < n; r0 += ROWS) {
         const int r = r0 + (lane & 15);
-        const bool live = r < rows.n;
-        i32x4 acc[P][NT];
-        accumulate<P, NT>(hd + (int64_t)(live ? rows.list[r] : 0) * P * I, I, live, b, I, acc);
-        share<P, NT>(acc, red);
-        for (int i = threadIdx.x; i < DOWN_COLS * ROWS; i += 256) {
-            const int row = i / DOWN_COLS, col = i % DOWN_COLS;
-            if (r0 + row >= rows.n || c0 + col >= H) continue;
-            const int at = col * ROWS + row;
-            float f = 0.f;
+        int exp_offset[4];
 #pragma unroll
-            for (int w = 0; w < 4; w++) f += red[w * NT * 16 * ROWS + at];
-            const int slot = rows.list[r0 + row];
-            part[(int64_t)slot * H + c0 + col] =
-                row_scaled(f, he[slot], a.dns[(int64_t)e * H + c0 + col]) * a.weights[slot];
+        for (int v = 0; v < 4; v++) {
+            const int q = r0 + 4 * (lane >> 4) + v;
+            exp_offset[v] = q < n ? 2 * rows[q] * row_exps : NONE;
+        }
+        float f[NT][4] = {};
+        stream<P, NT, WAVES / 2, true>(
+            hd, slots * P * I, r < n ? rows[r] * P * I : NONE, he, 2 * slots * row_exps, exp_offset, b, I, wave >> 1, ring0,
+            ring1, [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&ex)[4]) __attribute__((always_inline)) {
+                const i32x4 zero = {0, 0, 0, 0};
+                i32x4 acc[P][NT];
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int p = 0; p < P; p++)
+                        acc[p][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[p], fb[t], zero, 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int v = 0; v < 4; v++) f[t][v] += scaled_by(join<P, NT>(acc, t, v), ex[v]);
+            });
+        share_sums<NT>(f, ring0);
+        // a thread for each column and four rows
+        for (int i = threadIdx.x; i < DOWN_COLS * 4; i += THREADS) {
+            const int col = i % DOWN_COLS, q = i / DOWN_COLS, c = c0 + col;
+            if (r0 + 4 * q >= n || c >= H) continue;
+            float s[4];
+            shared_sum<NT, WAVES>(ring0, col >> 6, (col >> 4) & 3, q, col & 15, s);
+            const float sd = a.dns[(int64_t)e * H + c];
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                if (r0 + 4 * q + v >= n) break;
+                const int slot = rows[r0 + 4 * q + v];
+                const float y = s[v] * sd * a.weights[slot];
+                float* d = part + (int64_t)slot * H + c;
+                if (FEW) put(d, y);
+                else *d = y;
+            }
         }
         __syncthreads();
+    }
+    if (!FEW || !last_of(counts + slice, experts)) return;
+    const int quads = min(DOWN_COLS, H - c0) / 4;
+    for (int i = threadIdx.x; i < quads * (int)a.T; i += THREADS) {
+        const int t = i / quads, c = c0 + (i - t * quads) * 4;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (a.ids[t * k] >= 0) {
+            const float* p = part + (int64_t)t * k * H + c;
+#pragma unroll 8
+            for (int j = 0; j < k; j++, p += H) {
+                s.x += get(p);
+                s.y += get(p + 1);
+                s.z += get(p + 2);
+                s.w += get(p + 3);
+            }
+        }
+        store4<BF16>(a, t, c, s);
     }
 }
 
@@ -433,9 +705,7 @@ __global__ __launch_bounds__(256) void combine_kernel(MoeArgs a, const float* __
             s.z += v.z;
             s.w += v.w;
         }
-    char* y = static_cast<char*>(a.y) + (t * a.ldy + c) * (BF16 ? 2 : 4);
-    if (BF16) *reinterpret_cast<uint2*>(y) = make_uint2(to_bf16(s.x) | to_bf16(s.y) << 16, to_bf16(s.z) | to_bf16(s.w) << 16);
-    else *reinterpret_cast<float4*>(y) = s;
+    store4<BF16>(a, t, c, s);
 }
 
 template <bool BF16, int P>
@@ -444,15 +714,25 @@ hipError_t launch(const MoeArgs& a, hipStream_t s) {
     char* w = static_cast<char*>(a.ws);
     float* logits = reinterpret_cast<float*>(w + l.logits);
     int8_t *xd = reinterpret_cast<int8_t*>(w + l.xd), *hd = reinterpret_cast<int8_t*>(w + l.hd);
-    int *xe = reinterpret_cast<int*>(w + l.xe), *he = reinterpret_cast<int*>(w + l.he);
-    float *h = reinterpret_cast<float*>(w + l.h), *part = reinterpret_cast<float*>(w + l.part);
+    int* xe = reinterpret_cast<int*>(w + l.xe);
+    int16_t* he = reinterpret_cast<int16_t*>(w + l.he);
+    float* part = reinterpret_cast<float*>(w + l.part);
+    int* counts = reinterpret_cast<int*>(w + l.counts);
     const int64_t slots = a.T * a.topk, experts = a.E < slots ? a.E : slots;
-    const unsigned router = (unsigned)(a.T + ((a.E + 3) / 4) * ((a.T + 3) / 4));
-    router_kernel<BF16, P><<<router, 256, 0, s>>>(a, xd, xe, logits);
-    topk_kernel<<<(unsigned)a.T, 64, 0, s>>>(a, logits);
-    gate_up_kernel<P><<<(unsigned)(experts * ((a.I + UP_COLS - 1) / UP_COLS)), 256, 0, s>>>(a, xd, xe, h);
-    digits_kernel<P><<<(unsigned)slots, 256, 0, s>>>(a, h, hd, he);
-    down_kernel<P><<<(unsigned)(experts * ((a.H + DOWN_COLS - 1) / DOWN_COLS)), 256, 0, s>>>(a, hd, he, part);
+    const int64_t up = (a.I + UP_COLS - 1) / UP_COLS, down = (a.H + DOWN_COLS - 1) / DOWN_COLS;
+    // few: one workgroup a unit, of eight waves, which rank the logits themselves and add the slots themselves: what
+    // that takes is less than two more kernels (1 token, 64 experts of 2048 x 1024, 8 taken: 31 -> 27 us); past one
+    // workgroup a unit smaller ones and kernels of their own are faster (4 tokens: 61 -> 55 us)
+    const bool few = a.T * a.E <= RANKED && a.E <= RANKED_EXPERTS && experts * up < 2 * UNITS;
+    router_kernel<BF16, P><<<(unsigned)(a.T + a.E * ((a.T + 3) / 4)), 256, 0, s>>>(a, xd, xe, logits, counts, (int)down);
+    if (few) {
+        gate_up_kernel<P, 8, true><<<(unsigned)(experts * up + a.T), 512, 0, s>>>(a, xd, xe, logits, hd, he, (int)experts);
+        down_kernel<P, 8, true, BF16><<<(unsigned)(experts * down), 512, 0, s>>>(a, hd, he, part, counts, (int)experts);
+        return hipGetLastError();
+    }
+    topk_kernel<<<(unsigned)a.T, 256, 0, s>>>(a, logits);
+    gate_up_kernel<P, 4, false><<<(unsigned)(experts * up), 256, 0, s>>>(a, xd, xe, logits, hd, he, (int)experts);
+    down_kernel<P, 4, false, BF16><<<(unsigned)(experts * down), 256, 0, s>>>(a, hd, he, part, counts, (int)experts);
     combine_kernel<BF16><<<(unsigned)((a.T * (a.H / 4) + 255) / 256), 256, 0, s>>>(a, part);
     return hipGetLastError();
 }

@@ -2,8 +2,9 @@
 
 Bounds, element by element (u = 2^-24, half a step of fp32):
   x, h in fixed point   half a unit, 2^-23 (bf16) or 2^-31 (fp32) of the power of two above the row's largest
-  sums                  exact for each digit; digits and waves meet in at most 16 fp32 operations on values of
-                        at most 3 times the sum of magnitudes (signed digits), scales 3 more: 64 u of that sum
+  sums                  exact for each digit of a row of x, and of 64 neighbours of h; digits, waves and groups of 64
+                        meet in at most 16 + I / 64 fp32 operations on values of at most 3 times the sum of
+                        magnitudes (signed digits), scales 3 more: 64 u of that sum, and 3 I / 64 u more of h's
   silu(g) u             |silu'| <= 1.1; exp, quotient and products: 16 u
   slot weights          exp of a difference rounded to u |l_j - l_0|, sum and quotient: 64 u + 2 u |l_j - l_0|; below
                         2^-126 fp32 steps by 2^-149 whatever the size: exp (2 steps), quotient by a sum >= 1 (its
@@ -73,7 +74,7 @@ def reference(x, r, gu, gus, dn, dns, topk, renorm, active, dtype):
             hu = unit((np.abs(h) + dh)[None], P)[0]
             D, Sd = dn[e].astype(np.float64), dns[e].astype(np.float64)
             d = (D @ h) * Sd
-            dd = Sd * (np.abs(D) @ (dh + hu) + 64 * U * (np.abs(D) @ (np.abs(h) + dh + hu)))
+            dd = Sd * (np.abs(D) @ (dh + hu) + (64 + 3 * I / 64) * U * (np.abs(D) @ (np.abs(h) + dh + hu)))
             y[t] += p[t, j] * d
             bound[t] += p[t, j] * dd + dp[t, j] * np.abs(d) + (topk + 1) * U * p[t, j] * np.abs(d)
     bound += R.U_OUT[DT[dtype]] * (np.abs(y) + bound) + 1e-40
