@@ -385,11 +385,13 @@ struct Lines {
 };
 
 //
+// STREAMED: the codes by streaming copies, for many experts' weights (64 tokens over 128 experts 185 -> 170 us; a few
+// experts' may still be in the memory-side cache from the call before: one token 27 us against 29).
 // digits: row_offset is where this lane's row (l % 16) begins, or NONE.  EXPS: exponents too, one for each half block
 // of a row: exp_offset[v] is where those of row 4 (l / 16) + v begin, or NONE.
 constexpr int NONE = 0x40000000;   // past every buffer's end, and so is what is added to it: reads zeros
 
-template <int P, int NT, int SHARES, bool EXPS, class Use>
+template <int P, int NT, int SHARES, bool EXPS, bool STREAMED, class Use>
 __device__ __forceinline__ void stream(const int8_t* digits, int digits_bytes, int row_offset, const int16_t* exps,
                                        int exps_bytes, const int (&exp_offset)[4], const Lines (&b)[NT], int K, int share,
                                        char* ring0, char* ring1, Use use) {
@@ -418,7 +420,7 @@ __device__ __forceinline__ void stream(const int8_t* digits, int digits_bytes, i
 #pragma unroll
             for (int i = 0; i < 2; i++)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(ring + wave * SLOT + t * TILE + i * 1024), 16,
-                                                         at[i], 0, 0, 0);
+                                                         at[i], 0, 0, STREAMED ? 2 : 0);
         }
 #pragma unroll
         for (int s = 0; s < 2; s++) {
@@ -554,7 +556,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gate_up_kernel(MoeArgs a, const
         const int r = r0 + (lane & 15);
         i32x4 acc[P][NT] = {};
         const int none[4] = {NONE, NONE, NONE, NONE};
-        stream<P, NT, WAVES / 2, false>(
+        stream<P, NT, WAVES / 2, false, !FEW>(
             xd, T * P * H, r < n ? rows[r] / k * P * H : NONE, nullptr, 0, none, b, H, wave >> 1, ring0, ring1,
             [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&)[4]) __attribute__((always_inline)) {
 #pragma unroll
@@ -636,7 +638,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
             exp_offset[v] = q < n ? 2 * rows[q] * row_exps : NONE;
         }
         float f[NT][4] = {};
-        stream<P, NT, WAVES / 2, true>(
+        stream<P, NT, WAVES / 2, true, !FEW>(
             hd, slots * P * I, r < n ? rows[r] * P * I : NONE, he, 2 * slots * row_exps, exp_offset, b, I, wave >> 1, ring0,
             ring1, [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&ex)[4]) __attribute__((always_inline)) {
                 const i32x4 zero = {0, 0, 0, 0};
