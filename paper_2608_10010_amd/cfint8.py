@@ -15,8 +15,10 @@ from typing import Optional, Tuple
 import torch
 
 from . import curvefp as _cf
-from .curvefp import DTYPES, CurveFPError, _check, _matrix, _on_gpu, _source_arg, _stream
+from .curvefp import DTYPES, CurveFPError, _check, _device, _on_gpu, _source_arg, _stream
+from .curvefp import _matrix as _any_matrix
 
+_FLOATS = tuple(DTYPES)
 _fn = None
 
 
@@ -45,9 +47,34 @@ def lib() -> ctypes.CDLL:
 
 
 # ---------------------------------------------------------------- argument checks
+# A call takes about as long on the host as a small kernel on the GPU, so each check asks a tensor once for its shape
+# and strides and leaves the error's wording to the slow path.
+
+def _place(what: str, stream, **tensors):
+    """All tensors (None: absent) on the current GPU, and on the stream's when one is given."""
+    if stream is None:
+        dev = _device()
+        for t in tensors.values():
+            if t is not None and not (isinstance(t, torch.Tensor) and t.get_device() == dev):
+                break
+        else:
+            return
+    _on_gpu(what, [(name, t) for name, t in tensors.items() if t is not None], stream)
+
+
+def _matrix(what: str, name: str, t: torch.Tensor, rows: int, cols: int, dtypes):
+    """A 2-D row-major matrix of at least rows x cols."""
+    st, sh = t.stride(), t.shape
+    if len(st) == 2 and st[1] == 1 and sh[0] >= rows and sh[1] >= cols and (st[0] >= cols or rows == 1) \
+            and t.dtype in dtypes:
+        return
+    _any_matrix(what, name, t, rows, cols, dtypes)
+
 
 def _readable(what: str, name: str, t: torch.Tensor, rows: int, cols: int):
     """The last of the rows is readable up to the next multiple of 16 bytes (the others end in the next one)."""
+    if cols % 16 == 0:
+        return
     es = t.element_size()
     if (cols * es) % 16 == 0 or t.device.type == "meta":
         return
@@ -65,6 +92,8 @@ def _codes(what: str, name: str, t: torch.Tensor, rows: int, cols: int):
 
 def _vector(what: str, name: str, t: torch.Tensor, n: int, dtype=torch.float32):
     """A contiguous vector (any shape) of at least n values."""
+    if t.dtype is dtype and t.numel() >= n and t.is_contiguous():
+        return
     if t.dtype != dtype:
         raise ValueError(f"{what}: {name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
@@ -97,7 +126,7 @@ def _scratch(what, workspace, need: int, device, stream):
 def _ld(t: torch.Tensor, rows: int, cols: int) -> int:
     """Leading dimension of a matrix with 16-byte aligned rows; a single row has none of its own."""
     if rows > 1:
-        return t.stride(0)
+        return t.stride()[0]
     per = 16 // t.element_size()
     return -(-cols // per) * per
 
@@ -126,11 +155,7 @@ def cfint8_quantize(src: torch.Tensor, block_axis: int = 1, mul: Optional[torch.
     [rows, cols]; block_axis=0, a scale for each column, codes [cols, rows].  mul: fp32 factors along
     the quantized axis, multiplied in first."""
     what = "cfint8_quantize"
-    ts = [("src", src)]
-    for name, t in (("mul", mul), ("codes", codes), ("scales", scales), ("workspace", workspace)):
-        if t is not None:
-            ts.append((name, t))
-    _on_gpu(what, ts, stream)
+    _place(what, stream, src=src, mul=mul, codes=codes, scales=scales, workspace=workspace)
     _source_arg(what, src)
     rows, cols = src.shape
     outer, k = (rows, cols) if block_axis == 1 else (cols, rows)
@@ -159,16 +184,15 @@ def cfint8_dequantize(codes: torch.Tensor, scales: torch.Tensor, outer: int, k: 
                       dst: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """codes * scales, a scale for each row, as fp32 or bf16 (dst's dtype when it is given)."""
     what = "cfint8_dequantize"
-    ts = [("codes", codes), ("scales", scales)]
-    _on_gpu(what, ts if dst is None else ts + [("dst", dst)], stream)
+    _place(what, stream, codes=codes, scales=scales, dst=dst)
     _codes(what, "codes", codes, outer, k)
     _vector(what, "scales", scales, outer)
     if dst is None:
         if dtype not in DTYPES:
-            raise ValueError(f"{what}: dtype must be one of {tuple(DTYPES)}, got {dtype}")
+            raise ValueError(f"{what}: dtype must be one of {_FLOATS}, got {dtype}")
         per = 16 // dtype.itemsize
         dst = torch.empty((outer, -(-k // per) * per), dtype=dtype, device=codes.device)[:, :k]
-    _matrix(what, "dst", dst, outer, k, tuple(DTYPES))
+    _matrix(what, "dst", dst, outer, k, _FLOATS)
     st = lib().cfint8_dequantize(codes.data_ptr(), _ld(codes, outer, k), scales.data_ptr(), outer, k,
                                  dst.data_ptr(), DTYPES[dst.dtype], _ld(dst, outer, k), _stream(stream))
     _check(st, what)
@@ -186,12 +210,7 @@ def cfint8_gemm(a: torch.Tensor, a_scales: Optional[torch.Tensor], b: torch.Tens
     """C[M, N] = (a . b^T) a_scales[:, None] b_scales + bias in fp32 or bf16 (c's dtype when it is given).
     a: codes [M, K]; b: codes [N, K], or [K, N] with trans_b=1; scales of None are 1."""
     what = "cfint8_gemm"
-    ts = [("a", a), ("b", b)]
-    for name, t in (("a_scales", a_scales), ("b_scales", b_scales), ("bias", bias), ("c", c),
-                    ("workspace", workspace)):
-        if t is not None:
-            ts.append((name, t))
-    _on_gpu(what, ts, stream)
+    _place(what, stream, a=a, b=b, a_scales=a_scales, b_scales=b_scales, bias=bias, c=c, workspace=workspace)
     _codes(what, "a", a, M, K)
     if trans_b:
         _codes(what, "b", b, K, N)
@@ -205,13 +224,15 @@ def cfint8_gemm(a: torch.Tensor, a_scales: Optional[torch.Tensor], b: torch.Tens
         _vector(what, "bias", bias, N)
     if c is None:
         if dtype not in DTYPES:
-            raise ValueError(f"{what}: dtype must be one of {tuple(DTYPES)}, got {dtype}")
+            raise ValueError(f"{what}: dtype must be one of {_FLOATS}, got {dtype}")
         c = torch.empty((M, N), dtype=dtype, device=a.device)
     else:
-        _matrix(what, "c", c, M, N, tuple(DTYPES))
+        _matrix(what, "c", c, M, N, _FLOATS)
     L = lib()
-    wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_gemm_workspace_bytes, M, N, K, trans_b), a.device,
-                            stream)
+    wp, wb, held = None, 0, None
+    if trans_b or workspace is not None:             # otherwise the library needs none
+        wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_gemm_workspace_bytes, M, N, K, trans_b), a.device,
+                                stream)
     ldb = _ld(b, K, N) if trans_b else _ld(b, N, K)
     st = L.cfint8_gemm(a.data_ptr(), _ld(a, M, K), _ptr(a_scales), b.data_ptr(), ldb, trans_b, _ptr(b_scales),
                        _ptr(bias), M, N, K, c.data_ptr(), DTYPES[c.dtype], c.stride(0) if M > 1 else N, wp, wb,
@@ -233,12 +254,8 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
     [E, 2 I, H] with scales [E, 2 I], down codes [E, H, I] with scales [E, H].  active: uint8 or bool
     [T], 0 for padded tokens (zero rows, ids -1).  Returns y [T, H], ids int32 and weights fp32 [T, topk]."""
     what = "cfint8_moe"
-    ts = [("x", x), ("router", router), ("gate_up", gate_up), ("gate_up_scales", gate_up_scales), ("down", down),
-          ("down_scales", down_scales)]
-    for name, t in (("active", active), ("y", y), ("ids", ids), ("weights", weights), ("workspace", workspace)):
-        if t is not None:
-            ts.append((name, t))
-    _on_gpu(what, ts, stream)
+    _place(what, stream, x=x, router=router, gate_up=gate_up, gate_up_scales=gate_up_scales, down=down,
+           down_scales=down_scales, active=active, y=y, ids=ids, weights=weights, workspace=workspace)
     _source_arg(what, x)
     T, H = x.shape
     if router.dim() != 2 or router.shape[1] != H or router.dtype != x.dtype or not router.is_contiguous():
