@@ -7,6 +7,10 @@ failed check raising ValueError before anything reaches the library.
 
 Matrices of codes are 2-D int8 tensors whose row stride is a multiple of 16 bytes; a matrix of odd
 width is a view of a wider buffer (``codes_buffer``).
+
+``stream``: the call runs there instead of on the current stream, as if it stood inside
+``torch.cuda.stream(stream)``: outputs and workspaces that it allocates belong to that stream, and the
+caller orders the operands' earlier and later use on others.
 """
 
 import ctypes
@@ -109,14 +113,21 @@ def _bytes(what: str, fn, *args) -> int:
     return int(n)
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory that is first written on the call's stream comes from that stream's pool: a block of another one may
+    still be in use there by what its last owner queued."""
+    if stream is not None and device.type == "cuda":
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _scratch(what, workspace, need: int, device, stream):
-    """(pointer, bytes) of the workspace, allocated here when not given."""
+    """(pointer, bytes, tensor) of the workspace, allocated here when not given."""
     if workspace is None:
         if need == 0:
             return None, 0, None
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None and device.type == "cuda":
-            workspace.record_stream(stream)      # its memory goes back when this call returns
+        workspace = _empty((need,), torch.uint8, device, stream)
     have = workspace.numel() * workspace.element_size()
     if not workspace.is_contiguous() or have < need:
         raise ValueError(f"{what}: workspace must be contiguous and hold {need} bytes, it holds {have}")
@@ -135,10 +146,11 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def codes_buffer(rows: int, k: int, device) -> torch.Tensor:
-    """An uninitialised [rows, k] matrix of codes with rows of whole 16-byte pieces."""
+def codes_buffer(rows: int, k: int, device, stream=None) -> torch.Tensor:
+    """An uninitialised [rows, k] matrix of codes with rows of whole 16-byte pieces, for use on a stream (None: the
+    current one)."""
     ld = -(-k // 16) * 16
-    t = torch.empty((rows, ld), dtype=torch.int8, device=device)
+    t = _empty((rows, ld), torch.int8, torch.device(device), stream)
     return t if ld == k else t[:, :k]
 
 
@@ -162,11 +174,11 @@ def cfint8_quantize(src: torch.Tensor, block_axis: int = 1, mul: Optional[torch.
     if block_axis == 1:
         _readable(what, "src", src, rows, cols)
     if codes is None:
-        codes = codes_buffer(outer, k, src.device)
+        codes = codes_buffer(outer, k, src.device, stream)
     else:
         _matrix(what, "codes", codes, outer, k, (torch.int8,))
     if scales is None:
-        scales = torch.empty((outer,), dtype=torch.float32, device=src.device)
+        scales = _empty((outer,), torch.float32, src.device, stream)
     else:
         _vector(what, "scales", scales, outer)
     if mul is not None:
@@ -191,7 +203,7 @@ def cfint8_dequantize(codes: torch.Tensor, scales: torch.Tensor, outer: int, k: 
         if dtype not in DTYPES:
             raise ValueError(f"{what}: dtype must be one of {_FLOATS}, got {dtype}")
         per = 16 // dtype.itemsize
-        dst = torch.empty((outer, -(-k // per) * per), dtype=dtype, device=codes.device)[:, :k]
+        dst = _empty((outer, -(-k // per) * per), dtype, codes.device, stream)[:, :k]
     _matrix(what, "dst", dst, outer, k, _FLOATS)
     st = lib().cfint8_dequantize(codes.data_ptr(), _ld(codes, outer, k), scales.data_ptr(), outer, k,
                                  dst.data_ptr(), DTYPES[dst.dtype], _ld(dst, outer, k), _stream(stream))
@@ -225,7 +237,7 @@ def cfint8_gemm(a: torch.Tensor, a_scales: Optional[torch.Tensor], b: torch.Tens
     if c is None:
         if dtype not in DTYPES:
             raise ValueError(f"{what}: dtype must be one of {_FLOATS}, got {dtype}")
-        c = torch.empty((M, N), dtype=dtype, device=a.device)
+        c = _empty((M, N), dtype, a.device, stream)
     else:
         _matrix(what, "c", c, M, N, _FLOATS)
     L = lib()
@@ -275,15 +287,15 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
     if active is not None:
         _vector(what, "active", active, T, torch.bool if active.dtype == torch.bool else torch.uint8)
     if y is None:
-        y = torch.empty((T, H), dtype=x.dtype, device=x.device)
+        y = _empty((T, H), x.dtype, x.device, stream)
     else:
         _matrix(what, "y", y, T, H, (x.dtype,))
     if ids is None:
-        ids = torch.empty((T, topk), dtype=torch.int32, device=x.device)
+        ids = _empty((T, topk), torch.int32, x.device, stream)
     else:
         _vector(what, "ids", ids, T * topk, torch.int32)
     if weights is None:
-        weights = torch.empty((T, topk), dtype=torch.float32, device=x.device)
+        weights = _empty((T, topk), torch.float32, x.device, stream)
     else:
         _vector(what, "weights", weights, T * topk)
     L = lib()
