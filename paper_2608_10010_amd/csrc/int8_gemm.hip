@@ -3,13 +3,16 @@
 // C[m][n] = (sum_k qa[m][k] qb[n][k]) sa[m] sb[n] + bias[n]: v_mfma_i32_32x32x32_i8 sums exactly, so the
 // result depends neither on the tiling nor on the order of K, and every route gives the same C.
 //
-// tile_kernel: a workgroup of four waves owns a tile of 256 x 256 (or 128 x 128) outputs, a wave 128 x 128 (64 x 64) of it.
-// K goes in blocks of 128 codes, double-buffered in LDS by buffer-to-LDS loads; rows are 128 bytes with their
-// eight 16-byte pieces XOR-swizzled by row % 8 (applied to the addresses that the loads read), so the fragment
-// reads of 8 rows cover all banks.  A block's second half is read under the first half's MFMAs, the next
-// block's first half and the copy of the block after it go out under the second half's.  A 256 x 256 tile
-// needs 192 KB through the LDS a block (reads and copies) for 2048 cycles of MFMA, 75% of its rate;
-// smaller wave tiles would need more of it than there is.
+// tile_kernel: a workgroup of four waves owns a tile of 256 x 256 outputs (down to 64 x 64), a wave a quarter of it.
+// K goes in blocks of 128 codes through two to four stages of LDS, filled by buffer-to-LDS loads whose pieces of 16
+// codes are swizzled, so that the fragment reads cover all banks.  A block's second half is read under the first
+// half's MFMAs, the next block's first half and the copy of a later block go out under the second half's.  A
+// 256 x 256 tile needs 192 KB through the LDS a block (reads and copies) for 2048 cycles of MFMA, 75% of its rate;
+// smaller wave tiles would need more of it than there is.  At 8192 x 14336 x 4096 (437 us, 2200 TOPS) the matrix pipe
+// is busy for 74% of the cycles of a clock that the power limit holds at 1.67 GHz.
+//
+// An operand that lies as [K][N] goes to LDS in its own order and is turned by transposing reads on its way to
+// registers (4096 x 4096 x 14336 210 us against 235 with a pass that turns it first, 2048 x 2048 x 2048 14.6 against 21).
 #include <type_traits>
 
 #include "device_util.hpp"
@@ -22,6 +25,7 @@ using curvefp::u32x4;
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 // a piece of 16 codes without those past the first `left`
@@ -66,6 +70,10 @@ __device__ __forceinline__ float scaled(int sum, float sa, float sb, float bias)
     return ANY ? scaled_any(sum, sa, sb, bias) : (float)sum * (sa * sb) + bias;
 }
 
+__device__ __forceinline__ i32x2 read_tr(const char* p) {
+    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p);
+}
+
 // LDS written by some lanes of a wave is read by others behind this
 __device__ __forceinline__ void wave_exchange() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -95,12 +103,6 @@ __device__ __forceinline__ Tile tile_of(int b, int tiles_m, int tiles_n, int bm,
     return t;
 }
 
-// LDS has 64 banks of 4 bytes and serves 16 lanes of a 16-byte read at a time, here the same piece of 16 rows: two
-// rows of 128 bytes cover the banks, so the rows of equal parity take eight places (row / 2), a row of 256 covers them,
-// so all sixteen take their own.  (With row % 8 for rows of 128 half of the LDS's cycles were conflicts.)
-template <int BK>
-__device__ __forceinline__ int swizzle(int row) { return BK == 128 ? (row >> 1) & 7 : row & 15; }
-
 constexpr int BK = 128;   // codes of a block
 
 // LDS has 64 banks of 4 bytes and serves 16 lanes of a 16-byte read at a time, here the same piece of 16 rows: two
@@ -108,15 +110,22 @@ constexpr int BK = 128;   // codes of a block
 // LDS's cycles were conflicts.)
 __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 
-// TM, TN: MFMA tiles of 32 that a wave takes along M and N; S: stages
-template <int TM, int TN, int S, bool BF16>
+// The same for rows of BN bytes that hold B as [k][n]: a transposing read takes, for each half of a wave, 32 bytes of
+// eight rows, so these rows' 32-byte pairs of pieces take as many places as 256 bytes have.
+template <int BN>
+__device__ __forceinline__ int swizzle_kn(int row) { return BN == 256 ? row & 7 : BN == 128 ? (row >> 1) & 3 : (row >> 2) & 1; }
+
+constexpr int gcd(int a, int b) { return b == 0 ? a : gcd(b, a % b); }
+
+// TM, TN: MFMA tiles of 32 that a wave takes along M and N; S: stages; TRANS: b is [K][N]
+template <int TM, int TN, int S, bool BF16, bool TRANS>
 __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int tiles_n) {
     constexpr int BM = 64 * TM, BN = 64 * TN, WM = 32 * TM, WN = 32 * TN;
     constexpr int PIECES = BK / 16, COPY_ROWS = 1024 / BK;      // of a row; of a 1 KB copy
     constexpr int COPIES_A = BM * BK / 4096, COPIES_B = BN * BK / 4096;   // of a wave
     constexpr int SLICES = BK / 64;                             // 32 codes each, of half a block
-    constexpr int MFMAS = TM * TN * SLICES, READS = (TM + TN) * SLICES;   // of half a block
-    static_assert(COPIES_A + COPIES_B == READS, "one copy goes with each read");
+    constexpr int MFMAS = TM * TN * SLICES, READS = (TM + (TRANS ? 2 : 1) * TN) * SLICES;   // of half a block
+    constexpr int COPIES = COPIES_A + COPIES_B;
     constexpr int HALF = BM * BK;                               // where a stage's B begins
     constexpr int STAGE = HALF + BN * BK;
     __shared__ __attribute__((aligned(16))) char st0[STAGE], st1[STAGE], st2[S > 2 ? STAGE : 16], st3[S > 3 ? STAGE : 16];
@@ -146,12 +155,17 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
     // copies: a lane brings 16 bytes of its row, the piece that belongs where it writes; a row past the edge and a
     // piece past K lie behind the descriptor's end and arrive as zeros
     using lds_ptr = __attribute__((address_space(3))) void*;
-    const int8_t *A = g.a + m0 * g.lda, *B = g.b + n0 * g.ldb;
+    const int8_t *A = g.a + m0 * g.lda, *B = TRANS ? g.b + n0 : g.b + n0 * g.ldb;
     const int lda = (int)g.lda, ldb = (int)g.ldb, end_a = rows_a * lda, end_b = rows_b * ldb;
-    const int row_a = wave * COPIES_A * COPY_ROWS + lane / PIECES, row_b = wave * COPIES_B * COPY_ROWS + lane / PIECES;
+    constexpr int PIECES_B = TRANS ? BN / 16 : PIECES, COPY_ROWS_B = 64 / PIECES_B;
+    const int row_a = wave * COPIES_A * COPY_ROWS + lane / PIECES, row_b = wave * COPIES_B * COPY_ROWS_B + lane / PIECES_B;
     auto piece = [&](int i, int left) __attribute__((always_inline)) {   // of copy i; a wave's rows start at a multiple of 16
         const int p = 16 * ((lane % PIECES) ^ swizzle(i * COPY_ROWS + lane / PIECES));
         return p < left ? p : 0x40000000;
+    };
+    auto piece_kn = [&](int i) __attribute__((always_inline)) {   // a wave's rows start at a multiple of 8
+        const int p = 16 * ((lane % PIECES_B) ^ (2 * swizzle_kn<BN>(i * COPY_ROWS_B + lane / PIECES_B)));
+        return p < rows_b ? p : 0x40000000;
     };
     // past the last block descriptors of no bytes, so that every step counts the same loads
     auto copy = [&](int kb, char* st) __attribute__((always_inline)) {
@@ -160,7 +174,9 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
         const __amdgpu_buffer_rsrc_t ra =
             __builtin_amdgcn_make_buffer_rsrc((void*)(A + k), (short)0, in ? end_a - k : 0, 0x00020000);
         const __amdgpu_buffer_rsrc_t rb =
-            __builtin_amdgcn_make_buffer_rsrc((void*)(B + k), (short)0, in ? end_b - k : 0, 0x00020000);
+            TRANS ? __builtin_amdgcn_make_buffer_rsrc((void*)(B + (int64_t)k * ldb), (short)0,
+                                                      in ? min(K - k, BK) * ldb - (int)n0 : 0, 0x00020000)
+                  : __builtin_amdgcn_make_buffer_rsrc((void*)(B + k), (short)0, in ? end_b - k : 0, 0x00020000);
 #pragma unroll
         for (int i = 0; i < COPIES_A; i++) {
             const int at = row_a * lda + i * COPY_ROWS * lda + piece(i, K - k);
@@ -168,15 +184,17 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
         }
 #pragma unroll
         for (int i = 0; i < COPIES_B; i++) {
-            const int at = row_b * ldb + i * COPY_ROWS * ldb + piece(i, K - k);
+            const int at = row_b * ldb + i * COPY_ROWS_B * ldb + (TRANS ? piece_kn(i) : piece(i, K - k));
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(st + HALF + (wave * COPIES_B + i) * 1024), 16, at, 0,
                                                      0, 0);
         }
     };
-    static_assert((COPIES_A * COPY_ROWS) % 16 == 0 && (COPIES_B * COPY_ROWS) % 16 == 0, "rows of a wave's copies");
-    // K ends inside a piece of block kb, the last: A's codes behind it are cleared (B's then meet zeros)
+    static_assert((COPIES_A * COPY_ROWS) % 16 == 0 && (COPIES_B * COPY_ROWS_B) % (TRANS ? 8 : 16) == 0,
+                  "rows of a wave's copies");
+    // K ends inside a piece of block kb, the last: A's codes behind it are cleared (B's then meet zeros; rows of a
+    // [k][n] operand behind K are zeros already)
     auto clear_tail = [&](int kb, char* st) __attribute__((always_inline)) {
-        if (kb != nkb - 1 || K % 16 == 0) return;
+        if (TRANS || kb != nkb - 1 || K % 16 == 0) return;
         if (tid < BM) {
             const int at = K % BK, p = at >> 4;
             char* r = st + tid * BK + 16 * (p ^ swizzle(tid));
@@ -187,6 +205,18 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
 
     const int wm = wave >> 1, wn = wave & 1, lr = lane & 31;
     const int base_a = (wm * WM + lr) * BK, base_b = HALF + (wn * WN + lr) * BK;
+    // transposing read: 16 lanes give the addresses of 8 rows of 16 codes, two lanes a row, and get a column of 8 codes
+    // each; lanes 16 to 31 take the next 16 columns, lanes 32 to 63 the rows from 16 on, and a second read eight rows more
+    const int row_kn = 16 * (lane >> 5) + ((lane & 15) >> 1);
+    int at_kn[TN];
+    if constexpr (TRANS)
+#pragma unroll
+        for (int t = 0; t < TN; t++) {
+            at_kn[t] = row_kn * BN + 32 * ((wn * TN + t) ^ swizzle_kn<BN>(row_kn)) + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
+            // One offset of unknown origin: as a sum of parts the compiler loses track of which stage is read and waits
+            // for the copies into all of them
+            asm("" : "+v"(at_kn[t]));
+        }
     struct Half {
         i32x4 a[SLICES][TM], b[SLICES][TN];
     };
@@ -197,7 +227,16 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
 #pragma unroll
             for (int t = 0; t < TM; t++) f.a[s][t] = *reinterpret_cast<const i32x4*>(st + base_a + t * 32 * BK + off);
 #pragma unroll
-            for (int t = 0; t < TN; t++) f.b[s][t] = *reinterpret_cast<const i32x4*>(st + base_b + t * 32 * BK + off);
+            for (int t = 0; t < TN; t++) {
+                if constexpr (TRANS) {
+                    const char* r = st + at_kn[t];
+                    const int at = HALF + (64 * h + 32 * s) * BN;
+                    const i32x2 lo = read_tr(r + at), hi = read_tr(r + at + 8 * BN);
+                    f.b[s][t] = i32x4{lo.x, lo.y, hi.x, hi.y};
+                } else {
+                    f.b[s][t] = *reinterpret_cast<const i32x4*>(st + base_b + t * 32 * BK + off);
+                }
+            }
         }
     };
     i32x16 acc[TM][TN] = {};
@@ -208,7 +247,7 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
     };
     constexpr int SG_MFMA = 0x008, SG_VMEM = 0x010, SG_DSR = 0x100;
     // an even mix: GROUPS times (reads, copies, MFMAs)
-    constexpr int GROUPS = MFMAS < READS ? MFMAS : READS, RG = READS / GROUPS, MG = MFMAS / GROUPS;
+    constexpr int GROUPS = TRANS ? gcd(gcd(MFMAS, READS), COPIES) : MFMAS < READS ? MFMAS : READS, RG = READS / GROUPS, MG = MFMAS / GROUPS, CG = COPIES / GROUPS;
     auto phase1 = [&](Half& fa, Half& fb, char* st) __attribute__((always_inline)) {
         __builtin_amdgcn_s_waitcnt(0xC07F);   // fa's reads, a phase old
         load_half(fb, st, 1);
@@ -223,7 +262,7 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
     };
     // every wave is done with its stage, and the next block has landed: only S - 2 newer ones are still out
     // (vmcnt sits in bits 3:0 and 15:14, lgkmcnt in 11:8)
-    constexpr int OUT = (S - 2) * READS;
+    constexpr int OUT = (S - 2) * COPIES;
     static_assert(OUT < 64, "vmcnt holds 6 bits");
     auto handover = [&]() __attribute__((always_inline)) {
         asm volatile("" ::: "memory");
@@ -240,7 +279,7 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
 #pragma unroll
         for (int i = 0; i < GROUPS; i++) {
             __builtin_amdgcn_sched_group_barrier(SG_DSR, RG, 0);
-            __builtin_amdgcn_sched_group_barrier(SG_VMEM, RG, 0);
+            __builtin_amdgcn_sched_group_barrier(SG_VMEM, CG, 0);
             __builtin_amdgcn_sched_group_barrier(SG_MFMA, MG, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -260,7 +299,7 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
 #pragma unroll
         for (int d = 0; d < S; d++) copy(d, st[(F + d) % S]);
         asm volatile("" ::: "memory");
-        constexpr int LEFT = (S - 1) * READS;
+        constexpr int LEFT = (S - 1) * COPIES;
         static_assert(LEFT < 64, "vmcnt holds 6 bits");
         __builtin_amdgcn_s_waitcnt(0x0070 | (LEFT & 15) | ((LEFT >> 4) << 14));
         __builtin_amdgcn_s_barrier();
@@ -545,50 +584,83 @@ template <int TM, int TN, int S>
 hipError_t launch_tiles(const GemmArgs& g, hipStream_t s) {
     const int64_t tm = (g.M + 64 * TM - 1) / (64 * TM), tn = (g.N + 64 * TN - 1) / (64 * TN);
     const unsigned grid = (unsigned)(((tm * tn + 7) / 8) * 8);
-    if (g.c_bf16) tile_kernel<TM, TN, S, true><<<grid, 256, 0, s>>>(g, (int)tm, (int)tn);
-    else tile_kernel<TM, TN, S, false><<<grid, 256, 0, s>>>(g, (int)tm, (int)tn);
+    auto go = [&](auto bf16, auto trans) {
+        tile_kernel<TM, TN, S, decltype(bf16)::value, decltype(trans)::value><<<grid, 256, 0, s>>>(g, (int)tm, (int)tn);
+    };
+    if (g.trans) {
+        if (g.c_bf16) go(std::true_type{}, std::true_type{});
+        else go(std::false_type{}, std::true_type{});
+    } else {
+        if (g.c_bf16) go(std::true_type{}, std::false_type{});
+        else go(std::false_type{}, std::false_type{});
+    }
     return hipGetLastError();
 }
 
-// Route.  One or two rows against many columns load straight to registers: at least two workgroups for each unit cover
-// each other's waits (1 x 14336 x 4096 12.5 us against 13.2 through LDS; 1 x 4096 x 14336, one workgroup a unit, 14.9
-// against 12.0).  Up to 16 rows whose 16-column workgroups fit the units at once take these, eight waves where K gives
-// each at least two blocks (1 x 4096 x 14336 12.0 us against 15.9 with 32 x 32 tiles; 16 x 1024 x 1024 3.2 us against
-// 2.7 with four).  All else goes by the time of a tile's block of 128 codes and what a tile costs besides, as measured
-// with one tile on every unit (us; times with K = 4096: 256 x 256 67, 256 x 128 39, 128 x 128 23, 64 x 128 15.8,
-// 64 x 64 10.4, 32 x 32 6.6): the smaller tiles spend more on a product but fill the units with fewer rows.
-hipError_t launch_routed(const GemmArgs& g, hipStream_t s) {
-    auto tiles = [&](int64_t bm, int64_t bn) { return ((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
+// Route, by estimated time in us.  One or two rows against many columns load straight to registers: at least two
+// workgroups for each unit cover each other's waits (1 x 14336 x 4096 12.5 us against 13.2 through LDS; 1 x 4096 x 14336,
+// one workgroup a unit, 14.9 against 12.0).  Up to 16 rows whose 16-column workgroups fit the units at once take these,
+// eight waves where K gives each at least two blocks (1 x 4096 x 14336 12.0 us against 15.9 with 32 x 32 tiles; 16 x 1024
+// x 1024 3.2 us against 2.7 with four).  All else goes by the time of a tile's block of 128 codes and what a tile costs
+// besides, as measured with one tile on every unit (us; times with K = 4096: 256 x 256 67, 256 x 128 39, 128 x 128 23,
+// 64 x 128 15.8, 64 x 64 10.4, 32 x 32 6.6): the smaller tiles spend more on a product but fill the units with fewer rows.
+enum Kernel { ONE, FEW4, FEW8, FEW32, T64, T64_128, T128, T256_128, T256 };
+
+struct Route {
+    Kernel kernel;
+    double us;
+};
+
+// b [N][K], or [K][N] for the tile kernels
+Route route_direct(int64_t M, int64_t N, int64_t K, bool trans) {
     constexpr int64_t UNITS = 256;
-    if (g.M <= 2 && tiles(16, 16) >= 2 * UNITS) return launch_one<8, 8>(g, s);
-    if (g.M <= 16 && tiles(16, 16) <= UNITS)
-        return g.K >= 2048 ? launch_few<1, 1, 8>(g, s) : launch_few<1, 1, 4>(g, s);
-    const double blocks = (double)((g.K + 127) / 128);
+    auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    const double blocks = (double)((K + 127) / 128);
+    if (!trans && M <= 2 && tiles(16, 16) >= 2 * UNITS) return {ONE, 2.5 + (double)N * (double)K / 5e6};
+    if (!trans && M <= 16 && tiles(16, 16) <= UNITS) return {K >= 2048 ? FEW8 : FEW4, 2.5 + 0.07 * blocks};
     auto cost = [&](int64_t bm, int64_t bn, double once, double tile, double block) {
         return once + (double)((tiles(bm, bn) + UNITS - 1) / UNITS) * (tile + block * blocks);
     };
-    const double c[6] = {cost(32, 32, 2.5, 0.3, 0.11),  cost(64, 64, 2.0, 0.5, 0.235), cost(64, 128, 2.5, 1.0, 0.345),
-                         cost(128, 128, 0.0, 4.0, 0.59), cost(256, 128, 0.0, 6.0, 1.02), cost(256, 256, 0.0, 8.0, 1.83)};
-    int best = 0;
-    for (int i = 1; i < 6; i++)
-        if (c[i] < c[best]) best = i;
-    switch (best) {
-        case 0: return launch_few<2, 2, 4>(g, s);
-        case 1: return launch_tiles<1, 1, 4>(g, s);
-        case 2: return launch_tiles<1, 2, 3>(g, s);
-        case 3: return launch_tiles<2, 2, 3>(g, s);
-        case 4: return launch_tiles<4, 2, 3>(g, s);
+    const Route all[6] = {{FEW32, cost(32, 32, 2.5, 0.3, 0.11)},    {T64, cost(64, 64, 2.0, 0.5, trans ? 0.33 : 0.235)},
+                          {T64_128, cost(64, 128, 2.5, 1.0, 0.345)}, {T128, cost(128, 128, 0.0, 4.0, 0.59)},
+                          {T256_128, cost(256, 128, 0.0, 6.0, 1.02)}, {T256, cost(256, 256, 0.0, 8.0, 1.83)}};
+    int best = trans ? 1 : 0;
+    for (int i = best + 1; i < 6; i++)
+        if (all[i].us < all[best].us) best = i;
+    return all[best];
+}
+
+// A [K][N] operand is read as it lies, or turned into the workspace first, which costs a pass over it (at 4.4 TB/s) and a
+// launch but leaves the kernels that split K among the waves to few rows: with few columns (16 x 1024 x 4096 9.0 us against
+// 12.7 as it lies; 16 x 4096 x 14336 43 against 55, 16 x 4096 x 4096 16.0 against 11.9, 4096 x 4096 x 14336 235 against 210)
+bool turned(int64_t M, int64_t N, int64_t K) {
+    return 3.5 + (double)N * (double)K / 2.2e6 + route_direct(M, N, K, false).us < route_direct(M, N, K, true).us;
+}
+
+hipError_t launch_routed(const GemmArgs& g, hipStream_t s) {
+    switch (route_direct(g.M, g.N, g.K, g.trans).kernel) {
+        case ONE: return launch_one<8, 8>(g, s);
+        case FEW4: return launch_few<1, 1, 4>(g, s);
+        case FEW8: return launch_few<1, 1, 8>(g, s);
+        case FEW32: return launch_few<2, 2, 4>(g, s);
+        case T64: return launch_tiles<1, 1, 4>(g, s);
+        case T64_128: return launch_tiles<1, 2, 3>(g, s);
+        case T128: return launch_tiles<2, 2, 3>(g, s);
+        case T256_128: return launch_tiles<4, 2, 3>(g, s);
         default: return launch_tiles<4, 4, 2>(g, s);
     }
 }
 
 }  // namespace
 
-int64_t gemm_workspace_bytes(int64_t, int64_t N, int64_t K, int trans) { return trans ? N * ceil_to(K, 16) : 0; }
+int64_t gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int trans) {
+    return trans && turned(M, N, K) ? N * ceil_to(K, 16) : 0;
+}
 
 hipError_t launch_gemm(const GemmArgs& args, hipStream_t s) {
     GemmArgs g = args;
-    if (g.trans) {
+    if (g.trans && turned(g.M, g.N, g.K)) {
+        g.trans = 0;
         int8_t* t = static_cast<int8_t*>(g.ws);
         g.b = t;
         g.ldb = ceil_to(g.K, 16);

@@ -142,3 +142,17 @@ def test_results_do_not_depend_on_the_route():
         c = i8.cfint8_gemm(ta, ga, tb, gb, M, N, K)
         torch.cuda.synchronize()
         R.same_bits(c, whole[:M, :N], f"{M} x {N}")
+
+
+@pytest.mark.parametrize("M,N,K", [(600, 4096, 300), (1500, 2300, 4097), (2100, 4100, 1001), (4097, 4200, 259),
+                                   (16, 1030, 4100), (40, 200, 9000), (2, 9000, 530)])
+def test_transposed_operands_of_every_tile(M, N, K):
+    """The same product from [N][K] and from [K][N] codes, bit for bit."""
+    say(f"[int8 gemm] transposed {M} {N} {K}")
+    a, b, sa, sb, bs = case(M, N, K)
+    ta, tb, tt = R.codes_tensor(a, fill=5), R.codes_tensor(b, fill=9), R.codes_tensor(b.T, fill=-7)
+    for dtype in (torch.float32, torch.bfloat16):
+        want = i8.cfint8_gemm(ta, dev(sa), tb, dev(sb), M, N, K, bias=dev(bs), dtype=dtype)
+        got = i8.cfint8_gemm(ta, dev(sa), tt, dev(sb), M, N, K, trans_b=1, bias=dev(bs), dtype=dtype)
+        torch.cuda.synchronize()
+        R.same_bits(got, want.cpu(), f"{M}x{N}x{K}")
