@@ -147,9 +147,12 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def codes_buffer(rows: int, k: int, device, stream=None) -> torch.Tensor:
-    """An uninitialised [rows, k] matrix of codes with rows of whole 16-byte pieces, for use on a stream (None: the
-    current one)."""
+    """An uninitialised [rows, k] matrix of codes for use on a stream (None: the current one): contiguous where k is a
+    multiple of 16, otherwise with rows of whole 16-byte pieces, or of whole 128-byte lines of memory where these add
+    at most an eighth (a product reads rows by 128 codes: 333 x 6151 x 4099 20.8 us, 26.2 with rows of 4112 bytes)."""
     ld = -(-k // 16) * 16
+    if ld != k and -(-k // 128) * 128 - k <= k // 8:
+        ld = -(-k // 128) * 128
     t = _empty((rows, ld), torch.int8, torch.device(device), stream)
     return t if ld == k else t[:, :k]
 

@@ -9,7 +9,8 @@
 // half's MFMAs, the next block's first half and the copy of a later block go out under the second half's.  A
 // 256 x 256 tile needs 192 KB through the LDS a block (reads and copies) for 2048 cycles of MFMA, 75% of its rate;
 // smaller wave tiles would need more of it than there is.  At 8192 x 14336 x 4096 (437 us, 2200 TOPS) the matrix pipe
-// is busy for 74% of the cycles of a clock that the power limit holds at 1.67 GHz.
+// is busy for 74% of the cycles of a clock that the power limit holds at 1.67 GHz.  C goes past the caches that A and B
+// are read from (streaming stores: 415 us; no size measured loses more than 3%).
 //
 // An operand that lies as [K][N] goes to LDS in its own order and is turned by transposing reads on its way to
 // registers (4096 x 4096 x 14336 210 us against 235 with a pass that turns it first, 2048 x 2048 x 2048 14.6 against 21).
@@ -73,6 +74,9 @@ __device__ __forceinline__ float scaled(int sum, float sa, float sb, float bias)
 __device__ __forceinline__ i32x2 read_tr(const char* p) {
     return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p);
 }
+
+// 16 bytes of C at a multiple of an element's size
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
 // LDS written by some lanes of a wave is read by others behind this
 __device__ __forceinline__ void wave_exchange() {
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(256) void tile_kernel(GemmArgs g, int tiles_m, int 
                 if (mw + 32 * i + row >= g.M || nw + col >= g.N) continue;
                 char* d = C + ((32 * i + row) * g.ldc + col) * ES;
                 if (nw + col + 16 / ES <= g.N) {
-                    __builtin_memcpy(d, &v, 16);   // any alignment: ldc is the caller's
+                    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(d));   // any alignment: ldc is the caller's
                 } else {
                     for (int k = 0; k < 16 / ES; k++)
                         if (nw + col + k < g.N) {
