@@ -40,6 +40,9 @@ struct Layout {
 // exponents of a row of h: one for each 64 columns, an even number
 __host__ __device__ constexpr int64_t exponents(int64_t I) { return (I + 2 * UP_COLS - 1) / (2 * UP_COLS) * 2; }
 
+constexpr int ONE_COLS = 32;           // inner columns of a one-token gate_up workgroup: those of one exponent there
+__host__ __device__ constexpr int64_t one_exponents(int64_t I) { return (I + ONE_COLS - 1) / ONE_COLS; }
+
 Layout layout(int64_t T, int64_t E, int64_t topk, int64_t H, int64_t I) {
     Layout l;
     int64_t at = 0;
@@ -53,7 +56,7 @@ Layout layout(int64_t T, int64_t E, int64_t topk, int64_t H, int64_t I) {
     l.xd = take(T * 4 * H);
     l.xe = take(T * 4);
     l.hd = take(S * 4 * I);
-    l.he = take(S * exponents(I) * 2);
+    l.he = take(S * (T == 1 ? one_exponents(I) : exponents(I)) * 2);
     l.part = take(S * H * 4);
     l.counts = take((H + DOWN_COLS - 1) / DOWN_COLS * 4);   // arrivals of down's workgroups on each column slice
     l.bytes = at;
@@ -453,7 +456,8 @@ __device__ __forceinline__ void stream(const int8_t* digits, int digits_bytes, i
             for (int t = 0; t < NT; t++) fb[t] = *reinterpret_cast<const i32x4*>(st + t * TILE);
             int ex[4];
 #pragma unroll
-            for (int v = 0; v < 4; v++) ex[v] = EXPS ? (s ? x[v] >> 16 : (int16_t)x[v]) : 0;
+            for (int v = 0; v < 4; v++)   // a half block behind K has none: it was never written
+                ex[v] = !EXPS || 128 * (share + j * SHARES) + 64 * s >= K ? 0 : s ? x[v] >> 16 : (int16_t)x[v];
             use(f[s], fb, ex);
         }
     };
@@ -556,6 +560,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gate_up_kernel(MoeArgs a, const
         const int r = r0 + (lane & 15);
         i32x4 acc[P][NT] = {};
         const int none[4] = {NONE, NONE, NONE, NONE};
+        // what the epilogue multiplies with, on its way before the codes: there a wave takes four rows, a lane a column
+        const int c = c0 + lane, q = wave;
+        float sg = 0.f, su = 0.f;
+        int slot[4] = {}, ex[4] = {};
+        if (q < 4 && r0 + 4 * q < n) {
+            if (c < I) {
+                const float* s = a.gus + (int64_t)e * 2 * I + c;
+                sg = s[0], su = s[I];
+            }
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                slot[v] = rows[min(r0 + 4 * q + v, n - 1)];
+                ex[v] = xe[slot[v] / k];
+            }
+        }
         stream<P, NT, WAVES / 2, false, !FEW>(
             xd, T * P * H, r < n ? rows[r] / k * P * H : NONE, nullptr, 0, none, b, H, wave >> 1, ring0, ring1,
             [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&)[4]) __attribute__((always_inline)) {
@@ -571,29 +590,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gate_up_kernel(MoeArgs a, const
 #pragma unroll
             for (int v = 0; v < 4; v++) f[t][v] = join<P, NT>(acc, t, v);
         share_sums<NT>(f, ring0);
-        // a wave for each four rows, a lane for each column
-        const int c = c0 + lane, q = wave;
         if (q < 4 && r0 + 4 * q < n) {
-            float g[4], u[4], sg = 0.f, su = 0.f;
+            float g[4], u[4];
             shared_sum<NT, WAVES>(ring0, lane >> 5, (lane >> 4) & 1, q, lane & 15, g);
             shared_sum<NT, WAVES>(ring0, lane >> 5, 2 + ((lane >> 4) & 1), q, lane & 15, u);
-            if (c < I) {
-                const float* s = a.gus + (int64_t)e * 2 * I + c;
-                sg = s[0], su = s[I];
-            }
 #pragma unroll
             for (int v = 0; v < 4; v++) {
                 if (r0 + 4 * q + v >= n) break;
-                const int slot = rows[r0 + 4 * q + v], ex = xe[slot / k];
-                const float gv = row_scaled(g[v], ex, sg), uv = row_scaled(u[v], ex, su);
+                const float gv = row_scaled(g[v], ex[v], sg), uv = row_scaled(u[v], ex[v], su);
                 const float y = c < I ? gv / (1.f + expf(-gv)) * uv : 0.f;
                 const int eh = digit_exponent<P>(wave_max(__float_as_uint(y) & 0x7FFFFFFFu));
                 const uint32_t d = digits_of(y, eh);
-                int8_t* dst = hd + (int64_t)slot * P * I + c;
+                int8_t* dst = hd + (int64_t)slot[v] * P * I + c;
                 if (c < I)
 #pragma unroll
                     for (int p = 0; p < P; p++) dst[(int64_t)p * I] = (int8_t)(d >> (8 * p));
-                if (lane == 0) he[slot * exponents(I) + slice] = (int16_t)eh;
+                if (lane == 0) he[slot[v] * exponents(I) + slice] = (int16_t)eh;
             }
         }
         __syncthreads();
@@ -637,6 +649,20 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
             const int q = r0 + 4 * (lane >> 4) + v;
             exp_offset[v] = q < n ? 2 * rows[q] * row_exps : NONE;
         }
+        // as in gate_up; here a thread takes a column and four rows, and then the next four
+        constexpr int ROUNDS = DOWN_COLS * 4 / THREADS;
+        static_assert(THREADS % DOWN_COLS == 0, "a thread keeps its column");
+        const int col = threadIdx.x % DOWN_COLS, c = c0 + col;
+        int slot[ROUNDS][4];
+        float weight[ROUNDS][4];
+        const float sd = c < H ? a.dns[(int64_t)e * H + c] : 0.f;
+#pragma unroll
+        for (int i = 0; i < ROUNDS; i++)
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                slot[i][v] = rows[min(r0 + 4 * ((int)threadIdx.x / DOWN_COLS + THREADS / DOWN_COLS * i) + v, n - 1)];
+                weight[i][v] = a.weights[slot[i][v]];
+            }
         float f[NT][4] = {};
         stream<P, NT, WAVES / 2, true, !FEW>(
             hd, slots * P * I, r < n ? rows[r] * P * I : NONE, he, 2 * slots * row_exps, exp_offset, b, I, wave >> 1, ring0,
@@ -654,19 +680,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
                     for (int v = 0; v < 4; v++) f[t][v] += scaled_by(join<P, NT>(acc, t, v), ex[v]);
             });
         share_sums<NT>(f, ring0);
-        // a thread for each column and four rows
-        for (int i = threadIdx.x; i < DOWN_COLS * 4; i += THREADS) {
-            const int col = i % DOWN_COLS, q = i / DOWN_COLS, c = c0 + col;
+#pragma unroll
+        for (int i = 0; i < ROUNDS; i++) {
+            const int q = threadIdx.x / DOWN_COLS + THREADS / DOWN_COLS * i;
             if (r0 + 4 * q >= n || c >= H) continue;
             float s[4];
             shared_sum<NT, WAVES>(ring0, col >> 6, (col >> 4) & 3, q, col & 15, s);
-            const float sd = a.dns[(int64_t)e * H + c];
 #pragma unroll
             for (int v = 0; v < 4; v++) {
                 if (r0 + 4 * q + v >= n) break;
-                const int slot = rows[r0 + 4 * q + v];
-                const float y = s[v] * sd * a.weights[slot];
-                float* d = part + (int64_t)slot * H + c;
+                const float y = s[v] * sd * weight[i][v];
+                float* d = part + (int64_t)slot[i][v] * H + c;
                 if (FEW) put(d, y);
                 else *d = y;
             }
@@ -710,6 +734,197 @@ __global__ __launch_bounds__(256) void combine_kernel(MoeArgs a, const float* __
     store4<BF16>(a, t, c, s);
 }
 
+// ---------------------------------------------------------------- one token
+//
+// A token's experts share no weights, so a row of codes meets one row of digits: dot products of whole contiguous rows,
+// 16 codes a lane, v_dot4 for each digit, with every load of a workgroup on its way at once.  gate_up: a workgroup for each
+// (slot, 32 inner columns), a wave four of gate and of up.  down: a workgroup for each 8 output columns and all slots, a
+// wave a slot's 1024 inner columns at a time, so that no workgroup waits for another's sums.
+
+__device__ __forceinline__ uint32_t add_bits(uint32_t a, uint32_t b, int) { return a + b; }
+__device__ __forceinline__ uint32_t add_bits(uint32_t a, uint32_t b, float) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+}
+
+// sums over the lanes of four values: lanes 16 i .. of the result hold those of value 0, 2, 1, 3.  Swaps of lanes' halves
+// and quarters leave a register for each two and then four values, sixteen lanes are added by rotations
+template <class V>
+__device__ __forceinline__ V sum4(V a, V b, V c, V d) {
+    auto bits = [](V v) { return __builtin_bit_cast(uint32_t, v); };
+    const auto x = __builtin_amdgcn_permlane32_swap(bits(a), bits(b), false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(bits(c), bits(d), false, false);
+    const uint32_t ab = add_bits(x[0], x[1], V()), cd = add_bits(y[0], y[1], V());
+    const auto z = __builtin_amdgcn_permlane16_swap(ab, cd, false, false);
+    uint32_t s = add_bits(z[0], z[1], V());
+    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x128, 0xF, 0xF, false), V());
+    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x124, 0xF, 0xF, false), V());
+    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x122, 0xF, 0xF, false), V());
+    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x121, 0xF, 0xF, false), V());
+    return __builtin_bit_cast(V, s);
+}
+__device__ __forceinline__ int value_of_row(int row) { return row == 1 ? 2 : row == 2 ? 1 : row; }
+
+// digits . codes of a lane's 16
+template <int P>
+__device__ __forceinline__ void dots(const i32x4 (&d)[P], const i32x4& w, int (&acc)[P]) {
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int p = 0; p < P; p++) acc[p] = __builtin_amdgcn_sdot4(d[p][i], w[i], acc[p], false);
+}
+
+template <int P>
+__device__ __forceinline__ float join1(const int (&acc)[P]) {
+    float f = (float)acc[P - 1];
+#pragma unroll
+    for (int p = P - 2; p >= 0; p--) f = __builtin_fmaf(f, 256.f, (float)acc[p]);
+    return f;
+}
+
+// the token's slot-th expert, from its logits: a wave for each eight of 64 candidates counts the logits before theirs
+__device__ __forceinline__ int ranked(const float* __restrict__ logits, int E, int slot) {
+    __shared__ int expert;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t key[RANKED_EXPERTS / 64];
+#pragma unroll
+    for (int r = 0; r < RANKED_EXPERTS / 64; r++) key[r] = 64 * r + lane < E ? order_key(logits[64 * r + lane]) : 0;
+#pragma unroll
+    for (int r = 0; r < RANKED_EXPERTS / 64; r++) {
+        if (64 * r >= E) break;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int from = 8 * wave + i, e = 64 * r + from;
+            const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key[r], from);
+            int before = 0;
+#pragma unroll
+            for (int q = 0; q < RANKED_EXPERTS / 64; q++)
+                if (64 * q < E) before += __popcll(__ballot(key[q] > k || (key[q] == k && 64 * q + lane < e)));
+            if (before == slot && e < E && lane == 0) expert = e;
+        }
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(expert);
+}
+
+template <int P>
+__global__ __launch_bounds__(512) void gate_up_one_kernel(MoeArgs a, const int8_t* __restrict__ xd,
+                                                          const int* __restrict__ xe, const float* __restrict__ logits,
+                                                          int8_t* __restrict__ hd, int16_t* __restrict__ he) {
+    const int E = (int)a.E, H = (int)a.H, I = (int)a.I, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nsl = (int)one_exponents(I), slot = (int)blockIdx.x / nsl, slice = (int)blockIdx.x % nsl;
+    __shared__ __attribute__((aligned(16))) uint32_t keys[RANKED_EXPERTS];
+    __shared__ float sums[9], joined[2][ONE_COLS];
+    if (slot >= (int)a.topk) {   // the last workgroup: ids and weights for everyone else
+        if ((int)threadIdx.x < (E + 3) / 4 * 4) keys[threadIdx.x] = (int)threadIdx.x < E ? order_key(logits[threadIdx.x]) : 0;
+        __syncthreads();
+        take_topk<512>(a, 0, logits, keys, sums);
+        return;
+    }
+    if (a.active && !a.active[0]) return;
+    const int e = ranked(logits, E, slot), c0 = slice * ONE_COLS, cw = c0 + 4 * wave, c = c0 + lane;
+    const bool mine = wave == 0 && lane < ONE_COLS && c < I;
+    const float* s = a.gus + (int64_t)e * 2 * I + c;
+    const float sg = mine ? s[0] : 0.f, su = mine ? s[I] : 0.f;
+    const int ex = xe[0];
+    int acc[8][P] = {};
+    if (cw < I) {   // columns come in sixteens
+        const int8_t* w = a.gu + ((int64_t)e * 2 * I + cw) * H;
+        const __amdgpu_buffer_rsrc_t rg = __builtin_amdgcn_make_buffer_rsrc((void*)w, (short)0, 4 * H, 0x00020000);
+        const __amdgpu_buffer_rsrc_t ru =
+            __builtin_amdgcn_make_buffer_rsrc((void*)(w + (int64_t)I * H), (short)0, 4 * H, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc((void*)xd, (short)0, P * H, 0x00020000);
+        for (int k0 = 0; k0 < H; k0 += 2048) {
+            i32x4 d[2][P], v[2][8];
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const int k = k0 + 1024 * x + 16 * lane, at = k < H ? k : NONE;
+#pragma unroll
+                for (int p = 0; p < P; p++)
+                    d[x][p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rd, at + p * H, 0, 0));
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    v[x][r] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rg, at + r * H, 0, 0));
+                    v[x][4 + r] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ru, at + r * H, 0, 0));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);   // every load goes out before the first is waited for
+#pragma unroll
+            for (int x = 0; x < 2; x++)
+#pragma unroll
+                for (int r = 0; r < 8; r++) dots<P>(d[x], v[x][r], acc[r]);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; g++) {
+        int sum[P];
+#pragma unroll
+        for (int p = 0; p < P; p++)
+            sum[p] = sum4(acc[4 * g][p], acc[4 * g + 1][p], acc[4 * g + 2][p], acc[4 * g + 3][p]);
+        if ((lane & 15) == 0) joined[g][4 * wave + value_of_row(lane >> 4)] = join1<P>(sum);
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    float y = 0.f;
+    if (mine) {
+        const float gv = row_scaled(joined[0][lane], ex, sg), uv = row_scaled(joined[1][lane], ex, su);
+        y = gv / (1.f + expf(-gv)) * uv;
+    }
+    const int eh = digit_exponent<P>(wave_max(__float_as_uint(y) & 0x7FFFFFFFu));
+    const uint32_t q = digits_of(y, eh);
+    if (mine)
+#pragma unroll
+        for (int p = 0; p < P; p++) hd[(int64_t)(slot * P + p) * I + c] = (int8_t)(q >> (8 * p));
+    if (lane == 0) he[slot * nsl + slice] = (int16_t)eh;
+}
+
+template <int P, bool BF16>
+__global__ __launch_bounds__(512) void down_one_kernel(MoeArgs a, const int8_t* __restrict__ hd,
+                                                       const int16_t* __restrict__ he) {
+    constexpr int COLS = 8;
+    __shared__ float part[CFINT8_MOE_MAX_TOPK * CFINT8_MOE_MAX_WIDTH / 1024][COLS];
+    const int H = (int)a.H, I = (int)a.I, k = (int)a.topk, nch = (I + 1023) / 1024, items = k * nch, c0 = blockIdx.x * COLS;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row_exps = (int)one_exponents(I), col = value_of_row(lane >> 4);   // of the first four
+    const bool live = !a.active || a.active[0];
+    if (live)
+        for (int it = wave; it < items; it += 8) {
+            const int slot = it / nch, e = __builtin_amdgcn_readfirstlane(a.ids[slot]), at = it % nch * 1024 + 16 * lane;
+            const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(a.dn + ((int64_t)e * H + c0) * I), (short)0, COLS * I, 0x00020000);
+            const __amdgpu_buffer_rsrc_t rd =
+                __builtin_amdgcn_make_buffer_rsrc((void*)(hd + (int64_t)slot * P * I), (short)0, P * I, 0x00020000);
+            const int off = at < I ? at : NONE;
+            i32x4 d[P], v[COLS];
+#pragma unroll
+            for (int r = 0; r < COLS; r++)
+                v[r] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off + r * I, 0, 0));
+#pragma unroll
+            for (int p = 0; p < P; p++)
+                d[p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rd, off + p * I, 0, 0));
+            const int ex = at < I ? he[slot * row_exps + at / ONE_COLS] : 0;
+            const float* sd = a.dns + (int64_t)e * H + c0 + col;
+            const float s0 = sd[0], s1 = sd[4], weight = a.weights[slot];
+            __builtin_amdgcn_sched_barrier(0);
+            float f[COLS];
+#pragma unroll
+            for (int r = 0; r < COLS; r++) {
+                int acc[P] = {};
+                dots<P>(d, v[r], acc);
+                f[r] = scaled_by(join1<P>(acc), ex);
+            }
+            const float y0 = sum4(f[0], f[1], f[2], f[3]) * s0 * weight, y1 = sum4(f[4], f[5], f[6], f[7]) * s1 * weight;
+            if ((lane & 15) == 0) part[it][col] = y0, part[it][4 + col] = y1;
+        }
+    __syncthreads();
+    if (threadIdx.x >= COLS) return;
+    float s = 0.f;
+    if (live)
+        for (int it = 0; it < items; it++) s += part[it][threadIdx.x];
+    if (BF16) static_cast<uint16_t*>(a.y)[c0 + threadIdx.x] = (uint16_t)to_bf16(s);
+    else static_cast<float*>(a.y)[c0 + threadIdx.x] = s;
+}
+
 template <bool BF16, int P>
 hipError_t launch(const MoeArgs& a, hipStream_t s) {
     const Layout l = layout(a.T, a.E, a.topk, a.H, a.I);
@@ -725,6 +940,12 @@ hipError_t launch(const MoeArgs& a, hipStream_t s) {
     // few: one workgroup a unit, of eight waves, which rank the logits themselves and add the slots themselves: what
     // that takes is less than two more kernels (1 token, 64 experts of 2048 x 1024, 8 taken: 31 -> 27 us); past one
     // workgroup a unit smaller ones and kernels of their own are faster (4 tokens: 61 -> 55 us)
+    if (a.T == 1 && a.E <= RANKED_EXPERTS) {
+        router_kernel<BF16, P><<<(unsigned)(1 + a.E), 256, 0, s>>>(a, xd, xe, logits, counts, 0);
+        gate_up_one_kernel<P><<<(unsigned)(a.topk * one_exponents(a.I) + 1), 512, 0, s>>>(a, xd, xe, logits, hd, he);
+        down_one_kernel<P, BF16><<<(unsigned)(a.H / 8), 512, 0, s>>>(a, hd, he);
+        return hipGetLastError();
+    }
     const bool few = a.T * a.E <= RANKED && a.E <= RANKED_EXPERTS && experts * up < 2 * UNITS;
     router_kernel<BF16, P><<<(unsigned)(a.T + a.E * ((a.T + 3) / 4)), 256, 0, s>>>(a, xd, xe, logits, counts, (int)down);
     if (few) {

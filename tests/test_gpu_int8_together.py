@@ -282,14 +282,14 @@ def test_memory_allocated_for_another_stream():
         same([t.cpu() for t in got], [t.cpu() for t in want], "codes")
 
 
-@pytest.mark.parametrize("byte", [0, 0x7F, 0xFF])
-def test_workspaces_need_no_contents(byte):
-    say(f"[int8 together] workspaces of {byte}")
+@pytest.mark.parametrize("word", [0, 0x7F7F, -1, -0x8000])      # the last: an exponent that stands for NaN
+def test_workspaces_need_no_contents(word):
+    say(f"[int8 together] workspaces of {word}")
     work = Work(0)
     work.run()
     want = work.snapshot()
     for t in work.workspaces():
-        t.fill_(byte)
+        t.view(torch.int16).fill_(word)
     work.clear()
     work.run()
     same(work.snapshot(), want, "again")
