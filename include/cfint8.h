@@ -95,7 +95,7 @@ int cfint8_gemm(const int8_t* a, int64_t lda, const float* a_scales, const int8_
  *   g = (x[t] . gate_up[e][i]) s, u = (x[t] . gate_up[e][I + i]) s, h[i] = g / (1 + exp(-g)) u;
  *   y[t] = sum_j p[t][j] (h . down[e_j]) s, rounded once to x's dtype.
  * Codes enter the products exactly.  x and h enter them in fixed point, 22 bits (dtype bf16) or 30 bits (fp32)
- * below a power of two above the largest of a row of x or of 64 neighbours of h; the sums of up to 64 such
+ * below a power of two above the largest of a row of x or of up to 64 neighbours of h; the sums of up to 64 such
  * products (all of a row's for x) are exact, their order in fp32 depends on the sizes alone.
  *   x        [T][ld_x] of `dtype` (fp32 or bf16), 16-byte aligned rows; T in [1, CFINT8_MOE_MAX_TOKENS].
  *   router   [E][H] of `dtype`, 16-byte aligned; E in [1, CFINT8_MOE_MAX_EXPERTS].

@@ -273,38 +273,40 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
            down_scales=down_scales, active=active, y=y, ids=ids, weights=weights, workspace=workspace)
     _source_arg(what, x)
     T, H = x.shape
-    if router.dim() != 2 or router.shape[1] != H or router.dtype != x.dtype or not router.is_contiguous():
-        raise ValueError(f"{what}: router must be a contiguous [E, {H}] matrix of {x.dtype}, got "
-                         f"{tuple(router.shape)} {router.dtype}")
-    E = router.shape[0]
-    if down.dim() != 3 or down.shape[0] != E or down.shape[1] != H:
-        raise ValueError(f"{what}: down must be [{E}, {H}, I], got {tuple(down.shape)}")
-    I = down.shape[2]
-    if tuple(gate_up.shape) != (E, 2 * I, H):
-        raise ValueError(f"{what}: gate_up must be {(E, 2 * I, H)}, got {tuple(gate_up.shape)}")
-    for name, t in (("gate_up", gate_up), ("down", down)):
-        if t.dtype != torch.int8 or not t.is_contiguous():
-            raise ValueError(f"{what}: {name} must be contiguous torch.int8")
+    dtype, device = x.dtype, x.device
+    rs, ds, gs = router.shape, down.shape, gate_up.shape
+    if len(rs) != 2 or rs[1] != H or router.dtype != dtype or not router.is_contiguous():
+        raise ValueError(f"{what}: router must be a contiguous [E, {H}] matrix of {dtype}, got "
+                         f"{tuple(rs)} {router.dtype}")
+    E = rs[0]
+    if len(ds) != 3 or ds[0] != E or ds[1] != H:
+        raise ValueError(f"{what}: down must be [{E}, {H}, I], got {tuple(ds)}")
+    I = ds[2]
+    if gs != (E, 2 * I, H):
+        raise ValueError(f"{what}: gate_up must be {(E, 2 * I, H)}, got {tuple(gs)}")
+    if gate_up.dtype != torch.int8 or down.dtype != torch.int8 or not (gate_up.is_contiguous() and down.is_contiguous()):
+        name = "gate_up" if gate_up.dtype != torch.int8 or not gate_up.is_contiguous() else "down"
+        raise ValueError(f"{what}: {name} must be contiguous torch.int8")
     _vector(what, "gate_up_scales", gate_up_scales, E * 2 * I)
     _vector(what, "down_scales", down_scales, E * H)
     if active is not None:
         _vector(what, "active", active, T, torch.bool if active.dtype == torch.bool else torch.uint8)
     if y is None:
-        y = _empty((T, H), x.dtype, x.device, stream)
+        y = _empty((T, H), dtype, device, stream)
     else:
-        _matrix(what, "y", y, T, H, (x.dtype,))
+        _matrix(what, "y", y, T, H, (dtype,))
     if ids is None:
-        ids = _empty((T, topk), torch.int32, x.device, stream)
+        ids = _empty((T, topk), torch.int32, device, stream)
     else:
         _vector(what, "ids", ids, T * topk, torch.int32)
     if weights is None:
-        weights = _empty((T, topk), torch.float32, x.device, stream)
+        weights = _empty((T, topk), torch.float32, device, stream)
     else:
         _vector(what, "weights", weights, T * topk)
     L = lib()
-    wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_moe_workspace_bytes, T, E, topk, H, I), x.device,
+    wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_moe_workspace_bytes, T, E, topk, H, I), device,
                             stream)
-    st = L.cfint8_moe(x.data_ptr(), DTYPES[x.dtype], T, H, _ld(x, T, H), router.data_ptr(), E, gate_up.data_ptr(),
+    st = L.cfint8_moe(x.data_ptr(), DTYPES[dtype], T, H, _ld(x, T, H), router.data_ptr(), E, gate_up.data_ptr(),
                       gate_up_scales.data_ptr(), down.data_ptr(), down_scales.data_ptr(), I, topk,
                       1 if renormalize else 0, _ptr(active), y.data_ptr(), _ld(y, T, H), ids.data_ptr(),
                       weights.data_ptr(), wp, wb, _stream(stream))

@@ -7,14 +7,16 @@
 // product for each digit.  All sums of products are exact int32; the digits' sums meet in fp32.
 //
 //   router   logits in 64 bits (they decide, so they are right to the last bit); x into digits
-//   topk     a workgroup for each token: ids and weights (a few tokens: done by the next kernel's workgroups)
+// and, where the tokens' experts are mostly different ones (one token above all),
+//   gate_up_one  a workgroup for each (slot, 32 inner columns): ranks the token's logits itself, then dot products of
+//                whole rows; h as digits with a power of two for each such slice
+//   down_one     a workgroup for each (token, 8 output columns), all its slots
+// or else, each expert's codes read once for all its rows,
+//   topk     a workgroup for each token: ids and weights
 //   gate_up  a workgroup for each (expert, 64 inner columns): h, as digits with a power of two for each 64 of a row
 //            (so that no workgroup waits for a whole row's largest value)
 //   down     a workgroup for each (expert, 128 output columns): weighted partial rows, one for each slot
-//   combine  a token's slots added in order (few slots: by the last of down's workgroups on a column slice)
-//
-// What one workgroup leaves for another of the same kernel is stored and loaded past the XCDs' own caches (agent
-// scope), each thread waits for its stores before the workgroup counts itself in, and the last one loads only then.
+//   combine  a token's slots added in order
 #include "../../include/cfint8.h"
 #include "int8_internal.hpp"
 
@@ -27,21 +29,22 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 constexpr int POISON = INT16_MIN;      // exponent of values among which is a NaN or an infinity
 constexpr int ROWS = 16;               // token rows of a matrix product
 constexpr int64_t UNITS = 256;         // compute units
-constexpr int RANKED = 2048;           // logits that gate_up ranks itself ..
-constexpr int RANKED_EXPERTS = 256;    // .. over at most so many experts
+constexpr int RANKED_EXPERTS = 256;    // experts among which gate_up_one ranks
 constexpr int UP_COLS = 64;            // inner columns of a gate_up workgroup: h's columns of one exponent
 constexpr int DOWN_COLS = 128;         // output columns of a down workgroup
+constexpr int WAVES = 4;               // of either
 
 // workspace
 struct Layout {
-    int64_t logits, xd, xe, hd, he, part, counts, bytes;
+    int64_t logits, xd, xe, hd, he, part, bytes;
 };
 
 // exponents of a row of h: one for each 64 columns, an even number
 __host__ __device__ constexpr int64_t exponents(int64_t I) { return (I + 2 * UP_COLS - 1) / (2 * UP_COLS) * 2; }
 
-constexpr int ONE_COLS = 32;           // inner columns of a one-token gate_up workgroup: those of one exponent there
-__host__ __device__ constexpr int64_t one_exponents(int64_t I) { return (I + ONE_COLS - 1) / ONE_COLS; }
+// waves of a gate_up workgroup of the slot path, four inner columns each, which share an exponent there
+__host__ __device__ constexpr int one_waves(int P) { return P == 4 ? 4 : 8; }
+__host__ __device__ constexpr int64_t one_exponents(int64_t I, int P) { return (I + 4 * one_waves(P) - 1) / (4 * one_waves(P)); }
 
 Layout layout(int64_t T, int64_t E, int64_t topk, int64_t H, int64_t I) {
     Layout l;
@@ -56,9 +59,8 @@ Layout layout(int64_t T, int64_t E, int64_t topk, int64_t H, int64_t I) {
     l.xd = take(T * 4 * H);
     l.xe = take(T * 4);
     l.hd = take(S * 4 * I);
-    l.he = take(S * (T == 1 ? one_exponents(I) : exponents(I)) * 2);
+    l.he = take(S * (one_exponents(I, 4) + 2) * 2);   // enough for exponents() too
     l.part = take(S * H * 4);
-    l.counts = take((H + DOWN_COLS - 1) / DOWN_COLS * 4);   // arrivals of down's workgroups on each column slice
     l.bytes = at;
     return l;
 }
@@ -139,19 +141,16 @@ __device__ __forceinline__ void put_digits(const float* v, int e, int8_t* dst, i
     for (int p = 0; p < P; p++) *reinterpret_cast<uint2*>(dst + (int64_t)p * n + c) = d[p];
 }
 
-// workgroups [0, T): a token's x into digits (the first one clears the arrival counts too); then one for each
-// (expert, 4 tokens), its waves sharing H
+// workgroups [0, T): a token's x into digits; then one for each (expert, 4 tokens), its waves sharing H
 template <bool BF16, int P>
 __global__ __launch_bounds__(256) void router_kernel(MoeArgs a, int8_t* __restrict__ xd, int* __restrict__ xe,
-                                                     float* __restrict__ logits, int* __restrict__ counts, int ncounts) {
+                                                     float* __restrict__ logits) {
     __shared__ uint32_t top[4];
     __shared__ double part[4][4];
     const int T = (int)a.T, E = (int)a.E, H = (int)a.H, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t es = BF16 ? 2 : 4;
     int b = blockIdx.x;
     if (b < T) {
-        if (b == 0)
-            for (int i = threadIdx.x; i < ncounts; i += 256) counts[i] = 0;
         const char* src = static_cast<const char*>(a.x) + b * a.ldx * es;
         int8_t* dst = xd + (int64_t)b * P * H;
         uint32_t m = 0;
@@ -306,71 +305,6 @@ __device__ __forceinline__ int expert_of(const int32_t* __restrict__ ids, int i,
     return ids[i];
 }
 
-// Both at once from the logits (at most RANKED): the expert that index i stands for, or -1, and its rows.  A wave
-// for each token counts the logits before the expert's
-template <int WAVES>
-__device__ __forceinline__ int rank_rows(const MoeArgs& a, const uint32_t* keys, int stride, int i, uint16_t* list,
-                                         int& n) {
-    __shared__ int count;
-    __shared__ int expert;
-    __shared__ int16_t rank[256];
-    const int T = (int)a.T, E = (int)a.E, k = (int)a.topk, tid = threadIdx.x, lane = tid & 63;
-    int e = i, first = T;   // tokens before `first` must not take e
-    if (E > T * k) {
-        first = i / k;
-        if (a.active && !a.active[first]) return -1;
-        if (tid < E && rank_of(keys + first * stride, E, tid) == i - first * k) expert = tid;
-        __syncthreads();
-        e = expert;
-    }
-    for (int t = tid >> 6; t < T; t += WAVES) {
-        const uint32_t* q = keys + t * stride;
-        const uint32_t key = q[e];
-        int before = 0;
-        for (int j = lane; j < E; j += 64) before += q[j] > key || (q[j] == key && j < e);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
-        if (lane == 0) rank[t] = (int16_t)(before < k && (!a.active || a.active[t]) ? before : -1);
-    }
-    __syncthreads();
-    if (tid < 64) {
-        int found = 0;
-        for (int t0 = 0; t0 < T; t0 += 64) {
-            const int t = t0 + lane;
-            const bool hit = t < T && rank[t] >= 0;
-            const uint64_t b = __ballot(hit);
-            if (hit) list[found + __popcll(b & ((1ull << lane) - 1))] = (uint16_t)(t * k + rank[t]);
-            found += __popcll(b);
-        }
-        if (lane == 0) count = found;
-    }
-    __syncthreads();
-    n = count;
-    if (E > T * k && list[0] < first * k) return -1;   // an earlier token's workgroups have it
-    return e;
-}
-
-// this workgroup's arrival at a count that `all` workgroups reach: true in the last one.  Every thread's stores
-// have reached memory before the count does
-__device__ __forceinline__ bool last_of(int* count, int all) {
-    __shared__ int last;
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-    asm volatile("" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0)
-        last = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1;
-    __syncthreads();
-    return last != 0;
-}
-
-__device__ __forceinline__ void put(float* p, float v) {
-    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float get(const float* p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
 // Products of 16 rows x 16 NT columns over one of SHARES shares of K, in blocks of 128; use(row digits' fragments,
 // codes' fragments, exponents) takes them half a block at a time.  Codes go through LDS: loads of
 // 16 lines a quarter of a wave cost the L1 a lookup for each, 64 a kilobyte, copies of whole 128-byte pieces of
@@ -387,14 +321,12 @@ struct Lines {
     int lines;
 };
 
-//
-// STREAMED: the codes by streaming copies, for many experts' weights (64 tokens over 128 experts 185 -> 170 us; a few
-// experts' may still be in the memory-side cache from the call before: one token 27 us against 29).
+// The codes come by streaming copies (64 tokens over 128 experts 185 -> 170 us).
 // digits: row_offset is where this lane's row (l % 16) begins, or NONE.  EXPS: exponents too, one for each half block
 // of a row: exp_offset[v] is where those of row 4 (l / 16) + v begin, or NONE.
 constexpr int NONE = 0x40000000;   // past every buffer's end, and so is what is added to it: reads zeros
 
-template <int P, int NT, int SHARES, bool EXPS, bool STREAMED, class Use>
+template <int P, int NT, int SHARES, bool EXPS, class Use>
 __device__ __forceinline__ void stream(const int8_t* digits, int digits_bytes, int row_offset, const int16_t* exps,
                                        int exps_bytes, const int (&exp_offset)[4], const Lines (&b)[NT], int K, int share,
                                        char* ring0, char* ring1, Use use) {
@@ -423,7 +355,7 @@ __device__ __forceinline__ void stream(const int8_t* digits, int digits_bytes, i
 #pragma unroll
             for (int i = 0; i < 2; i++)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(ring + wave * SLOT + t * TILE + i * 1024), 16,
-                                                         at[i], 0, 0, STREAMED ? 2 : 0);
+                                                         at[i], 0, 0, 2);
         }
 #pragma unroll
         for (int s = 0; s < 2; s++) {
@@ -490,7 +422,7 @@ __device__ __forceinline__ void share_sums(const float (&f)[NT][4], char* ring0)
 }
 
 // rows 4 q .. 4 q + 3 of column c of tile t, over the waves that share these columns (every other one from `half`)
-template <int NT, int WAVES>
+template <int NT>
 __device__ __forceinline__ void shared_sum(const char* ring0, int half, int t, int q, int c, float (&out)[4]) {
     const char* at = ring0 + t * 1024 + 16 * (16 * q + c);
     float4 s = *reinterpret_cast<const float4*>(at + half * NT * TILE);
@@ -511,43 +443,22 @@ __device__ __forceinline__ float scaled_by(float f, int e) {
 }
 __device__ __forceinline__ float row_scaled(float f, int e, float s) { return scaled_by(f, e) * s; }
 
-// FEW: the logits are ranked here.  Waves of even number take the first 32 columns, the others the last
-template <int P, int WAVES, bool FEW>
+// Waves of even number take the first 32 columns, the others the last
+template <int P>
 __global__ __launch_bounds__(64 * WAVES, 2) void gate_up_kernel(MoeArgs a, const int8_t* __restrict__ xd,
-                                                             const int* __restrict__ xe,
-                                                             const float* __restrict__ logits,
-                                                             int8_t* __restrict__ hd, int16_t* __restrict__ he,
-                                                             int experts) {
-    constexpr int NT = 4, THREADS = 64 * WAVES;   // tiles: 2 of gate, 2 of up
-    __shared__ uint16_t lists[FEW ? 1 : WAVES][256];
+                                                                const int* __restrict__ xe, int8_t* __restrict__ hd,
+                                                                int16_t* __restrict__ he) {
+    constexpr int NT = 4;   // tiles: 2 of gate, 2 of up
+    __shared__ uint16_t lists[WAVES][256];
     __shared__ __attribute__((aligned(16))) char ring0[WAVES * NT * TILE], ring1[WAVES * NT * TILE];
     const int T = (int)a.T, E = (int)a.E, k = (int)a.topk, slots = T * k, H = (int)a.H, I = (int)a.I;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nsl = (I + UP_COLS - 1) / UP_COLS, index = (int)blockIdx.x / nsl;
-    uint16_t* rows = lists[FEW ? 0 : wave];
-    int e, n = 0;
-    if (FEW) {
-        __shared__ __attribute__((aligned(16))) uint32_t keys[RANKED + 4 * 256];
-        __shared__ float sums[WAVES + 1];
-        const int stride = (E + 3) / 4 * 4;
-        for (int i = threadIdx.x; i < T * stride; i += THREADS) {
-            const int t = i / stride, j = i - t * stride;
-            keys[i] = j < E ? order_key(logits[t * E + j]) : 0;
-        }
-        __syncthreads();
-        if (index >= experts) {   // the last T workgroups: a token's ids and weights for everyone else
-            const int t = (int)blockIdx.x - experts * nsl;
-            take_topk<THREADS>(a, t, logits, keys + t * stride, sums);
-            return;
-        }
-        e = rank_rows<WAVES>(a, keys, stride, index, rows, n);
-        if (e < 0 || n == 0) return;
-    } else {
-        e = expert_of(a.ids, index, slots, E);
-        if (e < 0) return;
-        n = find_rows(a.ids, slots, e, rows);
-        if (n == 0 || (E > slots && rows[0] != index)) return;
-    }
+    uint16_t* rows = lists[wave];
+    const int e = expert_of(a.ids, index, slots, E);
+    if (e < 0) return;
+    const int n = find_rows(a.ids, slots, e, rows);
+    if (n == 0 || (E > slots && rows[0] != index)) return;
     const int slice = (int)blockIdx.x % nsl, c0 = slice * UP_COLS, half = wave & 1;
     Lines b[NT];
 #pragma unroll
@@ -575,7 +486,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gate_up_kernel(MoeArgs a, const
                 ex[v] = xe[slot[v] / k];
             }
         }
-        stream<P, NT, WAVES / 2, false, !FEW>(
+        stream<P, NT, WAVES / 2, false>(
             xd, T * P * H, r < n ? rows[r] / k * P * H : NONE, nullptr, 0, none, b, H, wave >> 1, ring0, ring1,
             [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&)[4]) __attribute__((always_inline)) {
 #pragma unroll
@@ -592,8 +503,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gate_up_kernel(MoeArgs a, const
         share_sums<NT>(f, ring0);
         if (q < 4 && r0 + 4 * q < n) {
             float g[4], u[4];
-            shared_sum<NT, WAVES>(ring0, lane >> 5, (lane >> 4) & 1, q, lane & 15, g);
-            shared_sum<NT, WAVES>(ring0, lane >> 5, 2 + ((lane >> 4) & 1), q, lane & 15, u);
+            shared_sum<NT>(ring0, lane >> 5, (lane >> 4) & 1, q, lane & 15, g);
+            shared_sum<NT>(ring0, lane >> 5, 2 + ((lane >> 4) & 1), q, lane & 15, u);
 #pragma unroll
             for (int v = 0; v < 4; v++) {
                 if (r0 + 4 * q + v >= n) break;
@@ -619,11 +530,9 @@ __device__ __forceinline__ void store4(const MoeArgs& a, int t, int c, const flo
     else *reinterpret_cast<float4*>(y) = s;
 }
 
-// FEW: the last workgroup of a column slice adds the slots
-template <int P, int WAVES, bool FEW, bool BF16>
+template <int P>
 __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const int8_t* __restrict__ hd,
-                                                          const int16_t* __restrict__ he, float* part, int* counts,
-                                                          int experts) {
+                                                             const int16_t* __restrict__ he, float* __restrict__ part) {
     constexpr int NT = DOWN_COLS / 32, THREADS = 64 * WAVES;
     __shared__ uint16_t lists[WAVES][256];
     __shared__ __attribute__((aligned(16))) char ring0[WAVES * NT * TILE], ring1[WAVES * NT * TILE];
@@ -664,7 +573,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
                 weight[i][v] = a.weights[slot[i][v]];
             }
         float f[NT][4] = {};
-        stream<P, NT, WAVES / 2, true, !FEW>(
+        stream<P, NT, WAVES / 2, true>(
             hd, slots * P * I, r < n ? rows[r] * P * I : NONE, he, 2 * slots * row_exps, exp_offset, b, I, wave >> 1, ring0,
             ring1, [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&ex)[4]) __attribute__((always_inline)) {
                 const i32x4 zero = {0, 0, 0, 0};
@@ -685,34 +594,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
             const int q = threadIdx.x / DOWN_COLS + THREADS / DOWN_COLS * i;
             if (r0 + 4 * q >= n || c >= H) continue;
             float s[4];
-            shared_sum<NT, WAVES>(ring0, col >> 6, (col >> 4) & 3, q, col & 15, s);
+            shared_sum<NT>(ring0, col >> 6, (col >> 4) & 3, q, col & 15, s);
 #pragma unroll
             for (int v = 0; v < 4; v++) {
                 if (r0 + 4 * q + v >= n) break;
                 const float y = s[v] * sd * weight[i][v];
-                float* d = part + (int64_t)slot[i][v] * H + c;
-                if (FEW) put(d, y);
-                else *d = y;
+                part[(int64_t)slot[i][v] * H + c] = y;
             }
         }
         __syncthreads();
-    }
-    if (!FEW || !last_of(counts + slice, experts)) return;
-    const int quads = min(DOWN_COLS, H - c0) / 4;
-    for (int i = threadIdx.x; i < quads * (int)a.T; i += THREADS) {
-        const int t = i / quads, c = c0 + (i - t * quads) * 4;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (a.ids[t * k] >= 0) {
-            const float* p = part + (int64_t)t * k * H + c;
-#pragma unroll 8
-            for (int j = 0; j < k; j++, p += H) {
-                s.x += get(p);
-                s.y += get(p + 1);
-                s.z += get(p + 2);
-                s.w += get(p + 3);
-            }
-        }
-        store4<BF16>(a, t, c, s);
     }
 }
 
@@ -734,12 +624,14 @@ __global__ __launch_bounds__(256) void combine_kernel(MoeArgs a, const float* __
     store4<BF16>(a, t, c, s);
 }
 
-// ---------------------------------------------------------------- one token
+// ---------------------------------------------------------------- slot by slot
 //
-// A token's experts share no weights, so a row of codes meets one row of digits: dot products of whole contiguous rows,
+// One token's experts share no weights, so a row of codes meets one row of digits: dot products of whole contiguous rows,
 // 16 codes a lane, v_dot4 for each digit, with every load of a workgroup on its way at once.  gate_up: a workgroup for each
-// (slot, 32 inner columns), a wave four of gate and of up.  down: a workgroup for each 8 output columns and all slots, a
-// wave a slot's 1024 inner columns at a time, so that no workgroup waits for another's sums.
+// (slot, 32 inner columns), a wave four of gate and of up (fp32's fourth digit needs more registers: 16 columns, so that
+// three workgroups fit a unit; 7 tokens, 16 experts of 4096 x 2048 75 -> 70 us).  down: a workgroup for each (token, 8 output
+// columns), a wave a slot's 1024 inner columns at a time, so that no workgroup waits for another's sums.  Tokens on the
+// same expert read its codes from the L2 that they share.
 
 __device__ __forceinline__ uint32_t add_bits(uint32_t a, uint32_t b, int) { return a + b; }
 __device__ __forceinline__ uint32_t add_bits(uint32_t a, uint32_t b, float) {
@@ -782,6 +674,7 @@ __device__ __forceinline__ float join1(const int (&acc)[P]) {
 }
 
 // the token's slot-th expert, from its logits: a wave for each eight of 64 candidates counts the logits before theirs
+template <int W>
 __device__ __forceinline__ int ranked(const float* __restrict__ logits, int E, int slot) {
     __shared__ int expert;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -792,8 +685,8 @@ __device__ __forceinline__ int ranked(const float* __restrict__ logits, int E, i
     for (int r = 0; r < RANKED_EXPERTS / 64; r++) {
         if (64 * r >= E) break;
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int from = 8 * wave + i, e = 64 * r + from;
+        for (int i = 0; i < 64 / W; i++) {
+            const int from = 64 / W * wave + i, e = 64 * r + from;
             const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key[r], from);
             int before = 0;
 #pragma unroll
@@ -807,33 +700,38 @@ __device__ __forceinline__ int ranked(const float* __restrict__ logits, int E, i
 }
 
 template <int P>
-__global__ __launch_bounds__(512) void gate_up_one_kernel(MoeArgs a, const int8_t* __restrict__ xd,
+__global__ __launch_bounds__(64 * one_waves(P)) void gate_up_one_kernel(MoeArgs a, const int8_t* __restrict__ xd,
                                                           const int* __restrict__ xe, const float* __restrict__ logits,
                                                           int8_t* __restrict__ hd, int16_t* __restrict__ he) {
+    constexpr int W = one_waves(P), COLS = 4 * W;
     const int E = (int)a.E, H = (int)a.H, I = (int)a.I, lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nsl = (int)one_exponents(I), slot = (int)blockIdx.x / nsl, slice = (int)blockIdx.x % nsl;
+    const int T = (int)a.T, k = (int)a.topk, nsl = (int)one_exponents(I, P), slots = T * k;
     __shared__ __attribute__((aligned(16))) uint32_t keys[RANKED_EXPERTS];
-    __shared__ float sums[9], joined[2][ONE_COLS];
-    if (slot >= (int)a.topk) {   // the last workgroup: ids and weights for everyone else
-        if ((int)threadIdx.x < (E + 3) / 4 * 4) keys[threadIdx.x] = (int)threadIdx.x < E ? order_key(logits[threadIdx.x]) : 0;
+    __shared__ float sums[W + 1], joined[2][COLS];
+    const int grid = (nsl + 7) / 8 * 8 * slots;
+    if ((int)blockIdx.x >= grid) {   // the last T workgroups: a token's ids and weights for everyone else
+        const int t = (int)blockIdx.x - grid, i = threadIdx.x;
+        if (i < (E + 3) / 4 * 4) keys[i] = i < E ? order_key(logits[t * E + i]) : 0;
         __syncthreads();
-        take_topk<512>(a, 0, logits, keys, sums);
+        take_topk<64 * W>(a, t, logits, keys, sums);
         return;
     }
-    if (a.active && !a.active[0]) return;
-    const int e = ranked(logits, E, slot), c0 = slice * ONE_COLS, cw = c0 + 4 * wave, c = c0 + lane;
-    const bool mine = wave == 0 && lane < ONE_COLS && c < I;
+    // workgroups go to the 8 XCDs in turn: all slots of a column slice to one, whose L2 the tokens of an expert share
+    const int slot = ((int)blockIdx.x >> 3) % slots, slice = ((int)blockIdx.x >> 3) / slots * 8 + (blockIdx.x & 7), t = slot / k;
+    if (slice >= nsl || (a.active && !a.active[t])) return;
+    const int e = ranked<W>(logits + t * E, E, slot - t * k), c0 = slice * COLS, cw = c0 + 4 * wave, c = c0 + lane;
+    const bool mine = wave == 0 && lane < COLS && c < I;
     const float* s = a.gus + (int64_t)e * 2 * I + c;
     const float sg = mine ? s[0] : 0.f, su = mine ? s[I] : 0.f;
-    const int ex = xe[0];
+    const int ex = xe[t];
     int acc[8][P] = {};
     if (cw < I) {   // columns come in sixteens
         const int8_t* w = a.gu + ((int64_t)e * 2 * I + cw) * H;
         const __amdgpu_buffer_rsrc_t rg = __builtin_amdgcn_make_buffer_rsrc((void*)w, (short)0, 4 * H, 0x00020000);
         const __amdgpu_buffer_rsrc_t ru =
             __builtin_amdgcn_make_buffer_rsrc((void*)(w + (int64_t)I * H), (short)0, 4 * H, 0x00020000);
-        const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc((void*)xd, (short)0, P * H, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc((void*)(xd + (int64_t)t * P * H), (short)0, P * H, 0x00020000);
         for (int k0 = 0; k0 < H; k0 += 2048) {
             i32x4 d[2][P], v[2][8];
 #pragma unroll
@@ -875,7 +773,7 @@ __global__ __launch_bounds__(512) void gate_up_one_kernel(MoeArgs a, const int8_
     if (mine)
 #pragma unroll
         for (int p = 0; p < P; p++) hd[(int64_t)(slot * P + p) * I + c] = (int8_t)(q >> (8 * p));
-    if (lane == 0) he[slot * nsl + slice] = (int16_t)eh;
+    if (lane == 0) he[(int64_t)slot * nsl + slice] = (int16_t)eh;
 }
 
 template <int P, bool BF16>
@@ -883,13 +781,16 @@ __global__ __launch_bounds__(512) void down_one_kernel(MoeArgs a, const int8_t* 
                                                        const int16_t* __restrict__ he) {
     constexpr int COLS = 8;
     __shared__ float part[CFINT8_MOE_MAX_TOPK * CFINT8_MOE_MAX_WIDTH / 1024][COLS];
-    const int H = (int)a.H, I = (int)a.I, k = (int)a.topk, nch = (I + 1023) / 1024, items = k * nch, c0 = blockIdx.x * COLS;
+    const int H = (int)a.H, I = (int)a.I, k = (int)a.topk, nch = (I + 1023) / 1024, items = k * nch;
+    // as in gate_up, all tokens of a column slice to one XCD
+    const int t = ((int)blockIdx.x >> 3) % (int)a.T, c0 = (((int)blockIdx.x >> 3) / (int)a.T * 8 + (blockIdx.x & 7)) * COLS;
+    if (c0 >= H) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row_exps = (int)one_exponents(I), col = value_of_row(lane >> 4);   // of the first four
-    const bool live = !a.active || a.active[0];
+    const int row_exps = (int)one_exponents(I, P), col = value_of_row(lane >> 4);   // of the first four
+    const bool live = !a.active || a.active[t];
     if (live)
         for (int it = wave; it < items; it += 8) {
-            const int slot = it / nch, e = __builtin_amdgcn_readfirstlane(a.ids[slot]), at = it % nch * 1024 + 16 * lane;
+            const int slot = t * k + it / nch, e = __builtin_amdgcn_readfirstlane(a.ids[slot]), at = it % nch * 1024 + 16 * lane;
             const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
                 (void*)(a.dn + ((int64_t)e * H + c0) * I), (short)0, COLS * I, 0x00020000);
             const __amdgpu_buffer_rsrc_t rd =
@@ -902,7 +803,7 @@ __global__ __launch_bounds__(512) void down_one_kernel(MoeArgs a, const int8_t* 
 #pragma unroll
             for (int p = 0; p < P; p++)
                 d[p] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rd, off + p * I, 0, 0));
-            const int ex = at < I ? he[slot * row_exps + at / ONE_COLS] : 0;
+            const int ex = at < I ? he[slot * row_exps + at / (4 * one_waves(P))] : 0;
             const float* sd = a.dns + (int64_t)e * H + c0 + col;
             const float s0 = sd[0], s1 = sd[4], weight = a.weights[slot];
             __builtin_amdgcn_sched_barrier(0);
@@ -921,8 +822,27 @@ __global__ __launch_bounds__(512) void down_one_kernel(MoeArgs a, const int8_t* 
     float s = 0.f;
     if (live)
         for (int it = 0; it < items; it++) s += part[it][threadIdx.x];
-    if (BF16) static_cast<uint16_t*>(a.y)[c0 + threadIdx.x] = (uint16_t)to_bf16(s);
-    else static_cast<float*>(a.y)[c0 + threadIdx.x] = s;
+    const int64_t at = t * a.ldy + c0 + threadIdx.x;
+    if (BF16) static_cast<uint16_t*>(a.y)[at] = (uint16_t)to_bf16(s);
+    else static_cast<float*>(a.y)[at] = s;
+}
+
+// Slot by slot or expert by expert, by estimated time in us: three launches and their latencies, the weights of the
+// experts that T tokens take on average at 5.4 TB/s and those that slots share at 6.5, or 6 us for each 512
+// workgroups, which rank E logits first; or five launches and the experts' weights at 5.2 TB/s (fp32: 4.6).  (1 token, 8
+// of 64 experts of 2048 x 1024: 18 us against 40; 4 tokens 46 against 52; 12 tokens, 4 of 128 60 against 74; 16 tokens, 8
+// of 128 of 2048 x 768 107 against 102; 64 tokens, 2 of 16 103 against 45; fp32, 7 tokens, 2 of 16 of 4096 x 2048 68
+// against 77.)
+template <int P>
+bool by_slots(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I) {
+    if (E > RANKED_EXPERTS) return false;
+    const double weights = 3e-6 * (double)H * (double)I, slots = (double)(T * k);   // 1 MB takes 1 us at 1 TB/s
+    const double rounds = slots * (double)((I + 31) / 32) / (2.0 * UNITS), chunks = (double)((E + 63) / 64);
+    double untaken = 1;
+    for (int64_t t = 0; t < T; t++) untaken *= 1 - (double)k / (double)E;
+    const double taken = (double)E * (1 - untaken);
+    const double read = taken * weights / 5.4 + (slots - taken) * weights / 6.5;
+    return 10 + (read > 6 * rounds ? read : 6 * rounds) + 0.6 * rounds * chunks * chunks < 25 + taken * weights / (P == 4 ? 4.6 : 5.2);
 }
 
 template <bool BF16, int P>
@@ -934,28 +854,18 @@ hipError_t launch(const MoeArgs& a, hipStream_t s) {
     int* xe = reinterpret_cast<int*>(w + l.xe);
     int16_t* he = reinterpret_cast<int16_t*>(w + l.he);
     float* part = reinterpret_cast<float*>(w + l.part);
-    int* counts = reinterpret_cast<int*>(w + l.counts);
     const int64_t slots = a.T * a.topk, experts = a.E < slots ? a.E : slots;
     const int64_t up = (a.I + UP_COLS - 1) / UP_COLS, down = (a.H + DOWN_COLS - 1) / DOWN_COLS;
-    // few: one workgroup a unit, of eight waves, which rank the logits themselves and add the slots themselves: what
-    // that takes is less than two more kernels (1 token, 64 experts of 2048 x 1024, 8 taken: 31 -> 27 us); past one
-    // workgroup a unit smaller ones and kernels of their own are faster (4 tokens: 61 -> 55 us)
-    if (a.T == 1 && a.E <= RANKED_EXPERTS) {
-        router_kernel<BF16, P><<<(unsigned)(1 + a.E), 256, 0, s>>>(a, xd, xe, logits, counts, 0);
-        gate_up_one_kernel<P><<<(unsigned)(a.topk * one_exponents(a.I) + 1), 512, 0, s>>>(a, xd, xe, logits, hd, he);
-        down_one_kernel<P, BF16><<<(unsigned)(a.H / 8), 512, 0, s>>>(a, hd, he);
-        return hipGetLastError();
-    }
-    const bool few = a.T * a.E <= RANKED && a.E <= RANKED_EXPERTS && experts * up < 2 * UNITS;
-    router_kernel<BF16, P><<<(unsigned)(a.T + a.E * ((a.T + 3) / 4)), 256, 0, s>>>(a, xd, xe, logits, counts, (int)down);
-    if (few) {
-        gate_up_kernel<P, 8, true><<<(unsigned)(experts * up + a.T), 512, 0, s>>>(a, xd, xe, logits, hd, he, (int)experts);
-        down_kernel<P, 8, true, BF16><<<(unsigned)(experts * down), 512, 0, s>>>(a, hd, he, part, counts, (int)experts);
+    router_kernel<BF16, P><<<(unsigned)(a.T + a.E * ((a.T + 3) / 4)), 256, 0, s>>>(a, xd, xe, logits);
+    if (by_slots<P>(a.T, a.E, a.topk, a.H, a.I)) {
+        const int64_t slices = (one_exponents(a.I, P) + 7) / 8 * 8;
+        gate_up_one_kernel<P><<<(unsigned)(slices * slots + a.T), 64 * one_waves(P), 0, s>>>(a, xd, xe, logits, hd, he);
+        down_one_kernel<P, BF16><<<(unsigned)((a.H + 63) / 64 * 8 * a.T), 512, 0, s>>>(a, hd, he);
         return hipGetLastError();
     }
     topk_kernel<<<(unsigned)a.T, 256, 0, s>>>(a, logits);
-    gate_up_kernel<P, 4, false><<<(unsigned)(experts * up), 256, 0, s>>>(a, xd, xe, logits, hd, he, (int)experts);
-    down_kernel<P, 4, false, BF16><<<(unsigned)(experts * down), 256, 0, s>>>(a, hd, he, part, counts, (int)experts);
+    gate_up_kernel<P><<<(unsigned)(experts * up), 64 * WAVES, 0, s>>>(a, xd, xe, hd, he);
+    down_kernel<P><<<(unsigned)(experts * down), 64 * WAVES, 0, s>>>(a, hd, he, part);
     combine_kernel<BF16><<<(unsigned)((a.T * (a.H / 4) + 255) / 256), 256, 0, s>>>(a, part);
     return hipGetLastError();
 }

@@ -177,3 +177,34 @@ def test_zero_and_extreme_rows(dtype):
         x[3, 1:] = 0
 
     run(5, 5, 2, 96, 48, dtype, change=rows)
+
+
+# many rows on each expert, or more experts than one workgroup ranks: each expert's codes read once for all its rows
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,E,topk,H,I", [
+    (64, 16, 8, 64, 128), (256, 8, 4, 80, 48), (60, 12, 8, 272, 160), (256, 1, 1, 96, 528), (33, 260, 2, 64, 208),
+    (1, 300, 5, 48, 80), (100, 300, 3, 144, 64)])
+def test_expert_by_expert(T, E, topk, H, I, dtype):
+    run(T, E, topk, H, I, dtype, renorm=True, ldx=8 if dtype == "bf16" else 4)
+    active = np.ones(T, np.uint8)
+    active[T // 2:T // 2 + 3] = 0
+
+    def poison(x, r):
+        x[T // 2] = float("nan")
+
+    run(T, E, topk, H, I, dtype, renorm=False, seed=1, active=active, change=poison)
+
+
+def test_the_way_to_the_sums_does_not_matter():
+    """A token alone and in a batch large enough to go expert by expert: the same experts and weights, and outputs that
+    differ by no more than both bounds."""
+    T, E, topk, H, I = 80, 20, 4, 160, 288
+    say("[int8 moe] alone and in a batch")
+    x, r, gu, gus, dn, dns = make(T, E, H, I, "f32")
+    d = dev(x, r, gu, gus, dn, dns)
+    y, ids, w = i8.cfint8_moe(*d, topk)
+    Y, bound = reference(x, r, gu, gus, dn, dns, topk, True, None, "f32")[:2]
+    for t in (0, 41, 79):
+        y1, ids1, w1 = i8.cfint8_moe(d[0][t:t + 1], *d[1:], topk)
+        assert torch.equal(ids1[0], ids[t]) and torch.equal(w1[0], w[t])
+        assert (np.abs(y1[0].cpu().double().numpy() - y[t].cpu().double().numpy()) <= 2 * bound[t]).all()

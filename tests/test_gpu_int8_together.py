@@ -111,7 +111,8 @@ def test_moe_layer_on_quantized_weights():
 # ---------------------------------------------------------------- graphs, streams, workspaces
 
 SIZES = [(1, 4096, 520), (16, 256, 2048), (40, 96, 272), (200, 300, 400), (600, 1040, 256)]   # each kind of product
-LAYERS = [(1, 8, 2, 256, 128, BF), (20, 16, 4, 96, 64, F32), (64, 128, 4, 64, 48, BF)]
+LAYERS = [(1, 8, 2, 256, 128, BF), (20, 16, 4, 96, 64, F32), (64, 128, 4, 64, 48, BF), (40, 24, 8, 64, 160, F32),
+          (9, 260, 2, 80, 64, BF)]
 
 
 class Work:
