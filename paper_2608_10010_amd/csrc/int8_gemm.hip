@@ -18,6 +18,7 @@
 
 #include "device_util.hpp"
 #include "int8_internal.hpp"
+#include "int8_lanes.hpp"
 
 namespace cfint8 {
 
@@ -37,12 +38,6 @@ __device__ __forceinline__ i32x4 first_codes(i32x4 v, int left) {
         v[w] = b >= 4 ? v[w] : b <= 0 ? 0 : (int)((uint32_t)v[w] & ((1u << (8 * b)) - 1));
     }
     return v;
-}
-
-// the piece at p, of which the line holds `left` codes: zeros past them
-__device__ __forceinline__ i32x4 load16(const int8_t* p, int left) {
-    const i32x4 zero = {0, 0, 0, 0};
-    return left > 0 ? first_codes(*reinterpret_cast<const i32x4*>(p), left) : zero;
 }
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -392,55 +387,86 @@ __device__ __forceinline__ void store_few(const GemmArgs& g, i32x4 s, int64_t m,
     }
 }
 
-// One or two tokens against a weight: bound by the weight's codes, which go from memory through registers to the
-// matrix cores.  A workgroup owns 16 columns, its waves take the K blocks of 64 in turn and add their sums in LDS.
-// Lane l of a fragment is line l % 16, codes 16 (l / 16) .. of a block, what the lane loads itself; BATCH blocks
-// are requested before the first is used.
-template <int WAVES, int BATCH, bool BF16>
-__global__ __launch_bounds__(64 * WAVES) void one_kernel(GemmArgs g) {
-    __shared__ __attribute__((aligned(16))) i32x4 red[WAVES][64];
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
-    const int K = (int)g.K, kq = 16 * (lane >> 4), whole = K / 64;   // blocks that no lane's piece leaves
-    const int row = lane & 15;
-    const bool live = row < g.M;
-    const int8_t* a = g.a + (live ? row : 0) * g.lda + kq;
-    const int8_t* b = g.b + min(n0 + row, g.N - 1) * g.ldb + kq;
-    const i32x4 zero = {0, 0, 0, 0};
-    i32x4 acc = zero;
-    int kb = wave;
-    for (; kb + (BATCH - 1) * WAVES < whole; kb += BATCH * WAVES) {
-        i32x4 fa[BATCH], fb[BATCH];
+// One or two tokens against a weight: bound by the weight's codes.  A wave takes four columns, whose codes are four
+// contiguous lines, 16 codes a lane and load, against the tokens' by v_dot4; the next 2048 codes of each are requested
+// before these are used.
+template <int ROWS, bool BF16, bool STREAMED>
+__global__ __launch_bounds__(256) void dot_kernel(GemmArgs g) {
+    constexpr int COLS = 4, CHUNKS = 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = ((int64_t)blockIdx.x * 4 + wave) * COLS;
+    if (n0 >= g.N) return;
+    const int K = (int)g.K, lda = (int)g.lda, ldb = (int)g.ldb, used = (K + 15) & ~15;
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(g.b + n0 * g.ldb), (short)0, (int)(min((int64_t)COLS, g.N - n0) - 1) * ldb + used, 0x00020000);
+    const __amdgpu_buffer_rsrc_t ra =
+        __builtin_amdgcn_make_buffer_rsrc((void*)g.a, (short)0, ((int)g.M - 1) * lda + used, 0x00020000);
+    struct Chunk {
+        i32x4 a[CHUNKS][ROWS], b[CHUNKS][COLS];
+    };
+    auto request = [&](Chunk& f, int k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < BATCH; u++) {
-            const int k = (kb + u * WAVES) * 64;
-            fb[u] = *reinterpret_cast<const i32x4*>(b + k);
-            fa[u] = live ? *reinterpret_cast<const i32x4*>(a + k) : zero;
+        for (int x = 0; x < CHUNKS; x++) {
+            const int k = k0 + 1024 * x + 16 * lane;
+            const int at = k < K ? k : 0x40000000;   // behind the descriptors' ends: zeros
+#pragma unroll
+            for (int n = 0; n < COLS; n++)
+                f.b[x][n] = __builtin_bit_cast(
+                    i32x4, __builtin_amdgcn_raw_buffer_load_b128(rb, at + n * ldb, 0, STREAMED ? 2 : 0));
+#pragma unroll
+            for (int m = 0; m < ROWS; m++)
+                f.a[x][m] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, at + m * lda, 0, 0));
         }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int acc[ROWS][COLS] = {};
+    auto use = [&](Chunk& f, int k0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < BATCH; u++) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[u], fb[u], acc, 0, 0, 0);
-    }
-    for (; kb * 64 < K; kb += WAVES) {   // the rest, K's end among it
-        const int left = K - kb * 64 - kq;   // codes from this lane's piece on
-        const i32x4 fb = left > 0 ? *reinterpret_cast<const i32x4*>(b + kb * 64) : zero;
-        const i32x4 fa = live ? load16(a + kb * 64, left) : zero;
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa, fb, acc, 0, 0, 0);
-    }
-    red[wave][lane] = acc;
-    __syncthreads();
-    if (tid >= 64) return;
-    i32x4 s = red[0][tid];
+        for (int x = 0; x < CHUNKS; x++) {
+            if (k0 + 1024 * (x + 1) > K && K % 16 != 0)   // the piece that K ends in: whatever b holds there meets zeros
 #pragma unroll
-    for (int w = 1; w < WAVES; w++) s += red[w][tid];
-    store_few<BF16>(g, s, 4 * (tid >> 4), n0 + (tid & 15));   // element v of lane l: row 4 (l / 16) + v, column l % 16
+                for (int m = 0; m < ROWS; m++) f.a[x][m] = first_codes(f.a[x][m], K - k0 - 1024 * x - 16 * lane);
+#pragma unroll
+            for (int m = 0; m < ROWS; m++)
+#pragma unroll
+                for (int n = 0; n < COLS; n++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        acc[m][n] = __builtin_amdgcn_sdot4(f.a[x][m][i], f.b[x][n][i], acc[m][n], false);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    Chunk f0, f1;
+    constexpr int STEP = 1024 * CHUNKS;
+    request(f0, 0);
+    for (int k0 = 0; k0 < K; k0 += 2 * STEP) {
+        request(f1, k0 + STEP);
+        use(f0, k0);
+        request(f0, k0 + 2 * STEP);
+        use(f1, k0 + STEP);
+    }
+    const int64_t n = n0 + value_of_row(lane >> 4);
+    i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) s[m] = sum4(acc[m][0], acc[m][1], acc[m][2], acc[m][3]);
+    if ((lane & 15) == 0) store_few<BF16>(g, s, 0, n);
 }
 
-template <int WAVES, int BATCH>
-hipError_t launch_one(const GemmArgs& g, hipStream_t s) {
+// A weight of 100 MB or more is read past the memory-side cache (256 MB), as it will not be there for the next token
+// (1 x 28672 x 8192 36.8 us against 40.5, 1 x 32000 x 4096 22.3 against 23.6; 1 x 14336 x 4096 again and again 12.5 against 11.8)
+template <int ROWS>
+hipError_t launch_dot(const GemmArgs& g, hipStream_t s) {
     const unsigned grid = (unsigned)((g.N + 15) / 16);
-    if (g.c_bf16) one_kernel<WAVES, BATCH, true><<<grid, 64 * WAVES, 0, s>>>(g);
-    else one_kernel<WAVES, BATCH, false><<<grid, 64 * WAVES, 0, s>>>(g);
+    auto go = [&](auto bf16, auto streamed) {
+        dot_kernel<ROWS, decltype(bf16)::value, decltype(streamed)::value><<<grid, 256, 0, s>>>(g);
+    };
+    if (g.N * g.K >= 100000000) {
+        if (g.c_bf16) go(std::true_type{}, std::true_type{});
+        else go(std::false_type{}, std::true_type{});
+    } else {
+        if (g.c_bf16) go(std::true_type{}, std::false_type{});
+        else go(std::false_type{}, std::false_type{});
+    }
     return hipGetLastError();
 }
 
@@ -601,14 +627,17 @@ hipError_t launch_tiles(const GemmArgs& g, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Route, by estimated time in us.  One or two rows against many columns load straight to registers: at least two
-// workgroups for each unit cover each other's waits (1 x 14336 x 4096 12.5 us against 13.2 through LDS; 1 x 4096 x 14336,
-// one workgroup a unit, 14.9 against 12.0).  Up to 16 rows whose 16-column workgroups fit the units at once take these,
-// eight waves where K gives each at least two blocks (1 x 4096 x 14336 12.0 us against 15.9 with 32 x 32 tiles; 16 x 1024
-// x 1024 3.2 us against 2.7 with four).  All else goes by the time of a tile's block of 128 codes and what a tile costs
-// besides, as measured with one tile on every unit (us; times with K = 4096: 256 x 256 67, 256 x 128 39, 128 x 128 23,
-// 64 x 128 15.8, 64 x 64 10.4, 32 x 32 6.6): the smaller tiles spend more on a product but fill the units with fewer rows.
-enum Kernel { ONE, FEW4, FEW8, FEW32, T64, T64_128, T128, T256_128, T256 };
+// Route, by estimated time in us.  One or two rows take dot products of whole lines, except where K leaves much of a
+// wave's 2048 codes empty and there are workgroups of 16 columns for a part of the units only (1 x 14336 x 4096 12.7 us
+// against 13.4 through LDS, 1 x 28672 x 8192 40 against 49, 1 x 1000 x 4096 2.8 against 3.5; 2 x 512 x 512 2.7 against 2.3).
+// Up to 16 rows whose 16-column workgroups fit the units at once take these, eight waves where K gives each at least two
+// blocks (16 x 4096 x 14336 13.7 us against 17.7 with 32 x 32 tiles; 16 x 1024 x 1024 3.2 us against 2.7 with four), up to
+// 32 rows tiles of 32 x 32, which have more of the weight on its way than larger ones (16 x 14336 x 4096 13.9 us against
+// 15.8 with 64 x 64, 20 x 10000 x 1000 5.6 against 6.1).  All else goes by the time of a tile's block of 128 codes and what
+// a tile costs besides, as measured with one tile on every unit (us; times with K = 4096: 256 x 256 67, 256 x 128 39,
+// 128 x 128 23, 64 x 128 15.8, 64 x 64 10.4, 32 x 32 6.6): the smaller tiles spend more on a product but fill the units
+// with fewer rows.
+enum Kernel { DOT, FEW4, FEW8, FEW32, T64, T64_128, T128, T256_128, T256 };
 
 struct Route {
     Kernel kernel;
@@ -620,11 +649,12 @@ Route route_direct(int64_t M, int64_t N, int64_t K, bool trans) {
     constexpr int64_t UNITS = 256;
     auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     const double blocks = (double)((K + 127) / 128);
-    if (!trans && M <= 2 && tiles(16, 16) >= 2 * UNITS) return {ONE, 2.5 + (double)N * (double)K / 5e6};
+    if (!trans && M <= 2 && (K >= 2048 || tiles(16, 16) >= 2 * UNITS)) return {DOT, 2.5 + (double)N * (double)K / 5e6};
     if (!trans && M <= 16 && tiles(16, 16) <= UNITS) return {K >= 2048 ? FEW8 : FEW4, 2.5 + 0.07 * blocks};
     auto cost = [&](int64_t bm, int64_t bn, double once, double tile, double block) {
         return once + (double)((tiles(bm, bn) + UNITS - 1) / UNITS) * (tile + block * blocks);
     };
+    if (!trans && M <= 32) return {FEW32, cost(32, 32, 2.5, 0.3, 0.11)};
     const Route all[6] = {{FEW32, cost(32, 32, 2.5, 0.3, 0.11)},    {T64, cost(64, 64, 2.0, 0.5, trans ? 0.33 : 0.235)},
                           {T64_128, cost(64, 128, 2.5, 1.0, 0.345)}, {T128, cost(128, 128, 0.0, 4.0, 0.59)},
                           {T256_128, cost(256, 128, 0.0, 6.0, 1.02)}, {T256, cost(256, 256, 0.0, 8.0, 1.83)}};
@@ -643,7 +673,7 @@ bool turned(int64_t M, int64_t N, int64_t K) {
 
 hipError_t launch_routed(const GemmArgs& g, hipStream_t s) {
     switch (route_direct(g.M, g.N, g.K, g.trans).kernel) {
-        case ONE: return launch_one<8, 8>(g, s);
+        case DOT: return g.M == 1 ? launch_dot<1>(g, s) : launch_dot<2>(g, s);
         case FEW4: return launch_few<1, 1, 4>(g, s);
         case FEW8: return launch_few<1, 1, 8>(g, s);
         case FEW32: return launch_few<2, 2, 4>(g, s);

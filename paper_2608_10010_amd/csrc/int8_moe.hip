@@ -19,6 +19,7 @@
 //   combine  a token's slots added in order
 #include "../../include/cfint8.h"
 #include "int8_internal.hpp"
+#include "int8_lanes.hpp"
 
 namespace cfint8 {
 
@@ -632,29 +633,6 @@ __global__ __launch_bounds__(256) void combine_kernel(MoeArgs a, const float* __
 // three workgroups fit a unit; 7 tokens, 16 experts of 4096 x 2048 75 -> 70 us).  down: a workgroup for each (token, 8 output
 // columns), a wave a slot's 1024 inner columns at a time, so that no workgroup waits for another's sums.  Tokens on the
 // same expert read its codes from the L2 that they share.
-
-__device__ __forceinline__ uint32_t add_bits(uint32_t a, uint32_t b, int) { return a + b; }
-__device__ __forceinline__ uint32_t add_bits(uint32_t a, uint32_t b, float) {
-    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
-}
-
-// sums over the lanes of four values: lanes 16 i .. of the result hold those of value 0, 2, 1, 3.  Swaps of lanes' halves
-// and quarters leave a register for each two and then four values, sixteen lanes are added by rotations
-template <class V>
-__device__ __forceinline__ V sum4(V a, V b, V c, V d) {
-    auto bits = [](V v) { return __builtin_bit_cast(uint32_t, v); };
-    const auto x = __builtin_amdgcn_permlane32_swap(bits(a), bits(b), false, false);
-    const auto y = __builtin_amdgcn_permlane32_swap(bits(c), bits(d), false, false);
-    const uint32_t ab = add_bits(x[0], x[1], V()), cd = add_bits(y[0], y[1], V());
-    const auto z = __builtin_amdgcn_permlane16_swap(ab, cd, false, false);
-    uint32_t s = add_bits(z[0], z[1], V());
-    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x128, 0xF, 0xF, false), V());
-    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x124, 0xF, 0xF, false), V());
-    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x122, 0xF, 0xF, false), V());
-    s = add_bits(s, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x121, 0xF, 0xF, false), V());
-    return __builtin_bit_cast(V, s);
-}
-__device__ __forceinline__ int value_of_row(int row) { return row == 1 ? 2 : row == 2 ? 1 : row; }
 
 // digits . codes of a lane's 16
 template <int P>

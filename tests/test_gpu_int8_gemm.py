@@ -156,3 +156,10 @@ def test_transposed_operands_of_every_tile(M, N, K):
         got = i8.cfint8_gemm(ta, dev(sa), tt, dev(sb), M, N, K, trans_b=1, bias=dev(bs), dtype=dtype)
         torch.cuda.synchronize()
         R.same_bits(got, want.cpu(), f"{M}x{N}x{K}")
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 17, 2048), (2, 4099, 2050), (1, 5, 4095), (2, 3, 6000), (1, 70001, 1929), (2, 33000, 4100),
+                                   (1, 8195, 1), (3, 9000, 100), (32, 9001, 257)])
+def test_one_or_two_rows(M, N, K):
+    run(M, N, K)
+    run(M, N, K, dtype=torch.bfloat16, ld_extra=32, c_pad=5)
