@@ -54,31 +54,39 @@ def lib() -> ctypes.CDLL:
 # A call takes about as long on the host as a small kernel on the GPU, so each check asks a tensor once for its shape
 # and strides and leaves the error's wording to the slow path.
 
-def _place(what: str, stream, **tensors):
+def _place(what: str, stream, names, *tensors):
     """All tensors (None: absent) on the current GPU, and on the stream's when one is given."""
     if stream is None:
         dev = _device()
-        for t in tensors.values():
-            if t is not None and not (isinstance(t, torch.Tensor) and t.get_device() == dev):
-                break
-        else:
-            return
-    _on_gpu(what, [(name, t) for name, t in tensors.items() if t is not None], stream)
+        try:
+            for t in tensors:
+                if t is not None and t.get_device() != dev:
+                    break
+            else:
+                return
+        except AttributeError:                       # no tensor: the slow path says so
+            pass
+    _on_gpu(what, [(name, t) for name, t in zip(names, tensors) if t is not None], stream)
 
 
-def _matrix(what: str, name: str, t: torch.Tensor, rows: int, cols: int, dtypes):
-    """A 2-D row-major matrix of at least rows x cols."""
+_I8 = (torch.int8,)
+
+
+def _matrix(what: str, name: str, t: torch.Tensor, rows: int, cols: int, dtypes) -> int:
+    """A 2-D row-major matrix of at least rows x cols; its leading dimension (a single row of a matrix with 16-byte
+    aligned rows has none of its own)."""
     st, sh = t.stride(), t.shape
-    if len(st) == 2 and st[1] == 1 and sh[0] >= rows and sh[1] >= cols and (st[0] >= cols or rows == 1) \
-            and t.dtype in dtypes:
-        return
-    _any_matrix(what, name, t, rows, cols, dtypes)
+    if len(st) != 2 or st[1] != 1 or sh[0] < rows or sh[1] < cols or (st[0] < cols and rows != 1) or t.dtype not in dtypes:
+        _any_matrix(what, name, t, rows, cols, dtypes)
+        st = t.stride()
+    if rows > 1:
+        return st[0]
+    per = 16 // t.element_size()
+    return -(-cols // per) * per
 
 
 def _readable(what: str, name: str, t: torch.Tensor, rows: int, cols: int):
     """The last of the rows is readable up to the next multiple of 16 bytes (the others end in the next one)."""
-    if cols % 16 == 0:
-        return
     es = t.element_size()
     if (cols * es) % 16 == 0 or t.device.type == "meta":
         return
@@ -88,10 +96,12 @@ def _readable(what: str, name: str, t: torch.Tensor, rows: int, cols: int):
                          f"(a view of a wider buffer)")
 
 
-def _codes(what: str, name: str, t: torch.Tensor, rows: int, cols: int):
-    """A matrix of codes that is read."""
-    _matrix(what, name, t, rows, cols, (torch.int8,))
-    _readable(what, name, t, rows, cols)
+def _codes(what: str, name: str, t: torch.Tensor, rows: int, cols: int) -> int:
+    """A matrix of codes that is read; its leading dimension."""
+    ld = _matrix(what, name, t, rows, cols, _I8)
+    if cols % 16:
+        _readable(what, name, t, rows, cols)
+    return ld
 
 
 def _vector(what: str, name: str, t: torch.Tensor, n: int, dtype=torch.float32):
@@ -134,14 +144,6 @@ def _scratch(what, workspace, need: int, device, stream):
     return workspace.data_ptr(), have, workspace
 
 
-def _ld(t: torch.Tensor, rows: int, cols: int) -> int:
-    """Leading dimension of a matrix with 16-byte aligned rows; a single row has none of its own."""
-    if rows > 1:
-        return t.stride()[0]
-    per = 16 // t.element_size()
-    return -(-cols // per) * per
-
-
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -170,16 +172,19 @@ def cfint8_quantize(src: torch.Tensor, block_axis: int = 1, mul: Optional[torch.
     [rows, cols]; block_axis=0, a scale for each column, codes [cols, rows].  mul: fp32 factors along
     the quantized axis, multiplied in first."""
     what = "cfint8_quantize"
-    _place(what, stream, src=src, mul=mul, codes=codes, scales=scales, workspace=workspace)
+    _place(what, stream, ("src", "mul", "codes", "scales", "workspace"), src, mul, codes, scales, workspace)
     _source_arg(what, src)
     rows, cols = src.shape
-    outer, k = (rows, cols) if block_axis == 1 else (cols, rows)
+    ld_src = _matrix(what, "src", src, rows, cols, _FLOATS)
     if block_axis == 1:
-        _readable(what, "src", src, rows, cols)
+        outer, k = rows, cols
+        if cols % 16:
+            _readable(what, "src", src, rows, cols)
+    else:
+        outer, k = cols, rows
     if codes is None:
         codes = codes_buffer(outer, k, src.device, stream)
-    else:
-        _matrix(what, "codes", codes, outer, k, (torch.int8,))
+    ld_codes = _matrix(what, "codes", codes, outer, k, _I8)
     if scales is None:
         scales = _empty((outer,), torch.float32, src.device, stream)
     else:
@@ -187,10 +192,13 @@ def cfint8_quantize(src: torch.Tensor, block_axis: int = 1, mul: Optional[torch.
     if mul is not None:
         _vector(what, "mul", mul, k)
     L = lib()
-    need = 0 if block_axis == 1 else _bytes(what, L.cfint8_quantize_workspace_bytes, rows, cols, block_axis)
-    wp, wb, held = _scratch(what, workspace, need, src.device, stream)
-    st = L.cfint8_quantize(src.data_ptr(), DTYPES[src.dtype], rows, cols, _ld(src, rows, cols), block_axis, _ptr(mul),
-                           codes.data_ptr(), _ld(codes, outer, k), scales.data_ptr(), wp, wb, _stream(stream))
+    wp, wb, held = None, 0, None
+    if block_axis != 1 or workspace is not None:     # otherwise the library needs none
+        wp, wb, held = _scratch(what, workspace,
+                                _bytes(what, L.cfint8_quantize_workspace_bytes, rows, cols, block_axis), src.device,
+                                stream)
+    st = L.cfint8_quantize(src.data_ptr(), DTYPES[src.dtype], rows, cols, ld_src, block_axis, _ptr(mul),
+                           codes.data_ptr(), ld_codes, scales.data_ptr(), wp, wb, _stream(stream))
     _check(st, what)
     return codes, scales
 
@@ -199,17 +207,17 @@ def cfint8_dequantize(codes: torch.Tensor, scales: torch.Tensor, outer: int, k: 
                       dst: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """codes * scales, a scale for each row, as fp32 or bf16 (dst's dtype when it is given)."""
     what = "cfint8_dequantize"
-    _place(what, stream, codes=codes, scales=scales, dst=dst)
-    _codes(what, "codes", codes, outer, k)
+    _place(what, stream, ("codes", "scales", "dst"), codes, scales, dst)
+    ld_codes = _codes(what, "codes", codes, outer, k)
     _vector(what, "scales", scales, outer)
     if dst is None:
         if dtype not in DTYPES:
             raise ValueError(f"{what}: dtype must be one of {_FLOATS}, got {dtype}")
         per = 16 // dtype.itemsize
         dst = _empty((outer, -(-k // per) * per), dtype, codes.device, stream)[:, :k]
-    _matrix(what, "dst", dst, outer, k, _FLOATS)
-    st = lib().cfint8_dequantize(codes.data_ptr(), _ld(codes, outer, k), scales.data_ptr(), outer, k,
-                                 dst.data_ptr(), DTYPES[dst.dtype], _ld(dst, outer, k), _stream(stream))
+    ld_dst = _matrix(what, "dst", dst, outer, k, _FLOATS)
+    st = lib().cfint8_dequantize(codes.data_ptr(), ld_codes, scales.data_ptr(), outer, k, dst.data_ptr(),
+                                 DTYPES[dst.dtype], ld_dst, _stream(stream))
     _check(st, what)
     return dst
 
@@ -225,12 +233,10 @@ def cfint8_gemm(a: torch.Tensor, a_scales: Optional[torch.Tensor], b: torch.Tens
     """C[M, N] = (a . b^T) a_scales[:, None] b_scales + bias in fp32 or bf16 (c's dtype when it is given).
     a: codes [M, K]; b: codes [N, K], or [K, N] with trans_b=1; scales of None are 1."""
     what = "cfint8_gemm"
-    _place(what, stream, a=a, b=b, a_scales=a_scales, b_scales=b_scales, bias=bias, c=c, workspace=workspace)
-    _codes(what, "a", a, M, K)
-    if trans_b:
-        _codes(what, "b", b, K, N)
-    else:
-        _codes(what, "b", b, N, K)
+    _place(what, stream, ("a", "b", "a_scales", "b_scales", "bias", "c", "workspace"), a, b, a_scales, b_scales, bias, c,
+           workspace)
+    lda = _codes(what, "a", a, M, K)
+    ldb = _codes(what, "b", b, K, N) if trans_b else _codes(what, "b", b, N, K)
     if a_scales is not None:
         _vector(what, "a_scales", a_scales, M)
     if b_scales is not None:
@@ -241,17 +247,16 @@ def cfint8_gemm(a: torch.Tensor, a_scales: Optional[torch.Tensor], b: torch.Tens
         if dtype not in DTYPES:
             raise ValueError(f"{what}: dtype must be one of {_FLOATS}, got {dtype}")
         c = _empty((M, N), dtype, a.device, stream)
+        ldc = N
     else:
-        _matrix(what, "c", c, M, N, _FLOATS)
+        ldc = _matrix(what, "c", c, M, N, _FLOATS)
     L = lib()
     wp, wb, held = None, 0, None
     if trans_b or workspace is not None:             # otherwise the library needs none
         wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_gemm_workspace_bytes, M, N, K, trans_b), a.device,
                                 stream)
-    ldb = _ld(b, K, N) if trans_b else _ld(b, N, K)
-    st = L.cfint8_gemm(a.data_ptr(), _ld(a, M, K), _ptr(a_scales), b.data_ptr(), ldb, trans_b, _ptr(b_scales),
-                       _ptr(bias), M, N, K, c.data_ptr(), DTYPES[c.dtype], c.stride(0) if M > 1 else N, wp, wb,
-                       _stream(stream))
+    st = L.cfint8_gemm(a.data_ptr(), lda, _ptr(a_scales), b.data_ptr(), ldb, trans_b, _ptr(b_scales), _ptr(bias), M, N, K,
+                       c.data_ptr(), DTYPES[c.dtype], ldc, wp, wb, _stream(stream))
     _check(st, what)
     return c
 
@@ -269,10 +274,12 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
     [E, 2 I, H] with scales [E, 2 I], down codes [E, H, I] with scales [E, H].  active: uint8 or bool
     [T], 0 for padded tokens (zero rows, ids -1).  Returns y [T, H], ids int32 and weights fp32 [T, topk]."""
     what = "cfint8_moe"
-    _place(what, stream, x=x, router=router, gate_up=gate_up, gate_up_scales=gate_up_scales, down=down,
-           down_scales=down_scales, active=active, y=y, ids=ids, weights=weights, workspace=workspace)
+    _place(what, stream, ("x", "router", "gate_up", "gate_up_scales", "down", "down_scales", "active", "y", "ids",
+                          "weights", "workspace"),
+           x, router, gate_up, gate_up_scales, down, down_scales, active, y, ids, weights, workspace)
     _source_arg(what, x)
     T, H = x.shape
+    ld_x = _matrix(what, "x", x, T, H, _FLOATS)
     dtype, device = x.dtype, x.device
     rs, ds, gs = router.shape, down.shape, gate_up.shape
     if len(rs) != 2 or rs[1] != H or router.dtype != dtype or not router.is_contiguous():
@@ -293,8 +300,7 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
         _vector(what, "active", active, T, torch.bool if active.dtype == torch.bool else torch.uint8)
     if y is None:
         y = _empty((T, H), dtype, device, stream)
-    else:
-        _matrix(what, "y", y, T, H, (dtype,))
+    ld_y = _matrix(what, "y", y, T, H, (dtype,))
     if ids is None:
         ids = _empty((T, topk), torch.int32, device, stream)
     else:
@@ -306,9 +312,9 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
     L = lib()
     wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_moe_workspace_bytes, T, E, topk, H, I), device,
                             stream)
-    st = L.cfint8_moe(x.data_ptr(), DTYPES[dtype], T, H, _ld(x, T, H), router.data_ptr(), E, gate_up.data_ptr(),
+    st = L.cfint8_moe(x.data_ptr(), DTYPES[dtype], T, H, ld_x, router.data_ptr(), E, gate_up.data_ptr(),
                       gate_up_scales.data_ptr(), down.data_ptr(), down_scales.data_ptr(), I, topk,
-                      1 if renormalize else 0, _ptr(active), y.data_ptr(), _ld(y, T, H), ids.data_ptr(),
+                      1 if renormalize else 0, _ptr(active), y.data_ptr(), ld_y, ids.data_ptr(),
                       weights.data_ptr(), wp, wb, _stream(stream))
     _check(st, what)
     return y, ids, weights
