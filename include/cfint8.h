@@ -105,7 +105,8 @@ int cfint8_gemm(const int8_t* a, int64_t lda, const float* a_scales, const int8_
  *   active   null, or [T] bytes: a token whose byte is 0 (a padded one) takes no expert, reads no weight and
  *            gets a zero row, ids of -1 and weights of 0, whatever its x holds.
  *   y        [T][ld_y] of `dtype`, 16-byte aligned rows; ids int32 and weights fp32 [T][topk].
- *   workspace  at least cfint8_moe_workspace_bytes bytes, 256-byte aligned; scratch.
+ *   workspace  at least cfint8_moe_workspace_bytes bytes, 256-byte aligned; scratch, so calls that share it must be
+ *            ordered.
  * A NaN or an infinity in x gives NaN in that token's y (in no other's).
  * Errors: CURVEFP_ERR_NULL, _FORMAT (dtype), _SHAPE, _ALIGN, _HIP.
  */

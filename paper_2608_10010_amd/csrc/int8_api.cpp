@@ -85,8 +85,6 @@ int cfint8_gemm(const int8_t* a, int64_t lda, const float* a_scales, const int8_
     if (trans_b != 0 && trans_b != 1) return CURVEFP_ERR_BLOCK;
     if (!gemm_sizes_ok(M, N, K)) return CURVEFP_ERR_SHAPE;
     if (!ld_ok(lda, K) || !ld_ok(ldb, trans_b ? N : K) || ldc < N || ldc >= kMaxExtent) return CURVEFP_ERR_SHAPE;
-    // one workgroup for each tile of at least 16 x 16, numbered in 31 bits
-    if (((M + 15) / 16) * ((N + 15) / 16) >= kMaxExtent) return CURVEFP_ERR_SHAPE;
     const int64_t need = gemm_workspace_bytes(M, N, K, trans_b);
     if (need > 0 && !workspace) return CURVEFP_ERR_NULL;
     if (workspace_bytes < need) return CURVEFP_ERR_SHAPE;

@@ -703,7 +703,21 @@ hipError_t launch_gemm(const GemmArgs& args, hipStream_t s) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    return launch_routed(g, s);
+    const GemmArgs all = g;
+    hipError_t e = hipSuccess;
+    for (int64_t m = 0; m < all.M && e == hipSuccess; m += PART)
+        for (int64_t n = 0; n < all.N && e == hipSuccess; n += PART) {
+            g.M = all.M - m < PART ? all.M - m : PART;
+            g.N = all.N - n < PART ? all.N - n : PART;
+            g.a = all.a + m * all.lda;
+            g.b = all.b + (g.trans ? n : n * all.ldb);
+            g.as = all.as ? all.as + m : nullptr;
+            g.bs = all.bs ? all.bs + n : nullptr;
+            g.bias = all.bias ? all.bias + n : nullptr;
+            g.c = static_cast<char*>(all.c) + (m * all.ldc + n) * (all.c_bf16 ? 2 : 4);
+            e = launch_routed(g, s);
+        }
+    return e;
 }
 
 }  // namespace cfint8

@@ -6,6 +6,9 @@
 
 namespace cfint8 {
 
+// A launch has fewer than 2^32 threads: operands of more lines go in parts of so many
+constexpr int64_t PART = (int64_t)1 << 21;
+
 int64_t quantize_workspace_bytes(int64_t rows, int64_t cols, int axis);
 hipError_t launch_quantize(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, int axis,
                            const float* mul, int8_t* codes, int64_t ldq, float* scales, void* ws, hipStream_t s);

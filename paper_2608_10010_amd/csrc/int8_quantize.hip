@@ -30,7 +30,6 @@ namespace {
 
 constexpr uint32_t INF_BITS = 0x7F800000u;
 
-
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -535,33 +534,46 @@ int64_t quantize_workspace_bytes(int64_t rows, int64_t cols, int axis) {
 hipError_t launch_quantize(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, int axis,
                            const float* mul, int8_t* codes, int64_t ldq, float* scales, void* ws, hipStream_t s) {
     const bool bf16 = dtype == 1;
-    if (axis == 1) {
-        if (bf16) return mul ? launch_rows<true, true>(src, rows, cols, ld, mul, codes, ldq, scales, s)
-                             : launch_rows<true, false>(src, rows, cols, ld, mul, codes, ldq, scales, s);
-        return mul ? launch_rows<false, true>(src, rows, cols, ld, mul, codes, ldq, scales, s)
-                   : launch_rows<false, false>(src, rows, cols, ld, mul, codes, ldq, scales, s);
-    }
-    const bool al = reinterpret_cast<uintptr_t>(src) % 16 == 0 && (ld * (bf16 ? 2 : 4)) % 16 == 0;
-#define CFINT8_COLS(B, M, A) launch_cols<B, M, A>(src, rows, cols, ld, mul, codes, ldq, scales, ws, s)
-    if (bf16) {
-        if (mul) return al ? CFINT8_COLS(true, true, true) : CFINT8_COLS(true, true, false);
-        return al ? CFINT8_COLS(true, false, true) : CFINT8_COLS(true, false, false);
-    }
-    if (mul) return al ? CFINT8_COLS(false, true, true) : CFINT8_COLS(false, true, false);
-    return al ? CFINT8_COLS(false, false, true) : CFINT8_COLS(false, false, false);
+    const int64_t es = bf16 ? 2 : 4, lines = axis == 1 ? rows : cols;
+    const bool al = reinterpret_cast<uintptr_t>(src) % 16 == 0 && (ld * es) % 16 == 0;
+    hipError_t e = hipSuccess;
+    for (int64_t l = 0; l < lines && e == hipSuccess; l += PART) {
+        const int64_t n = lines - l < PART ? lines - l : PART;
+        const char* p = static_cast<const char*>(src) + (axis == 1 ? l * ld : l) * es;
+#define CFINT8_ROWS(B, M) launch_rows<B, M>(p, n, cols, ld, mul, codes + l * ldq, ldq, scales + l, s)
+#define CFINT8_COLS(B, M, A) launch_cols<B, M, A>(p, rows, n, ld, mul, codes + l * ldq, ldq, scales + l, ws, s)
+        if (axis == 1) {
+            if (bf16) e = mul ? CFINT8_ROWS(true, true) : CFINT8_ROWS(true, false);
+            else e = mul ? CFINT8_ROWS(false, true) : CFINT8_ROWS(false, false);
+        } else if (bf16) {
+            if (mul) e = al ? CFINT8_COLS(true, true, true) : CFINT8_COLS(true, true, false);
+            else e = al ? CFINT8_COLS(true, false, true) : CFINT8_COLS(true, false, false);
+        } else {
+            if (mul) e = al ? CFINT8_COLS(false, true, true) : CFINT8_COLS(false, true, false);
+            else e = al ? CFINT8_COLS(false, false, true) : CFINT8_COLS(false, false, false);
+        }
+#undef CFINT8_ROWS
 #undef CFINT8_COLS
+    }
+    return e;
 }
 
 hipError_t launch_dequantize(const int8_t* codes, int64_t ldq, const float* scales, int64_t outer, int64_t k, void* dst,
                              int dtype, int64_t ld, hipStream_t s) {
     const int width = (int)(k < SEG ? k : SEG);
     const int per = k >= SEG ? 1 : (int)(SEG / k > 64 ? 64 : SEG / k);
-    const dim3 grid((unsigned)((outer + per - 1) / per), (unsigned)((k + SEG - 1) / SEG));
     const Div32 d = make_div32((uint32_t)((width + 3) / 4));
-    char* p = static_cast<char*>(dst);
-    if (dtype == 1) dequantize_kernel<true><<<grid, 256, 0, s>>>(codes, ldq, scales, outer, k, p, ld, per, d, width);
-    else dequantize_kernel<false><<<grid, 256, 0, s>>>(codes, ldq, scales, outer, k, p, ld, per, d, width);
-    return hipGetLastError();
+    hipError_t e = hipSuccess;
+    for (int64_t l = 0; l < outer && e == hipSuccess; l += PART) {
+        const int64_t n = outer - l < PART ? outer - l : PART;
+        const dim3 grid((unsigned)((n + per - 1) / per), (unsigned)((k + SEG - 1) / SEG));
+        const int8_t* q = codes + l * ldq;
+        char* p = static_cast<char*>(dst) + l * ld * (dtype == 1 ? 2 : 4);
+        if (dtype == 1) dequantize_kernel<true><<<grid, 256, 0, s>>>(q, ldq, scales + l, n, k, p, ld, per, d, width);
+        else dequantize_kernel<false><<<grid, 256, 0, s>>>(q, ldq, scales + l, n, k, p, ld, per, d, width);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace cfint8

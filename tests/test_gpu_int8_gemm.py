@@ -163,3 +163,9 @@ def test_transposed_operands_of_every_tile(M, N, K):
 def test_one_or_two_rows(M, N, K):
     run(M, N, K)
     run(M, N, K, dtype=torch.bfloat16, ld_extra=32, c_pad=5)
+
+
+@pytest.mark.parametrize("M,N,trans", [((1 << 21) + 70, 3, 0), ((1 << 21) + 70, 20, 1), (1, (1 << 21) + 33, 0),
+                                       (3, (1 << 21) + 33, 0), (70, (1 << 21) + 65, 1)])
+def test_more_lines_than_a_launch_takes(M, N, trans):
+    run(M, N, 19, trans=trans)

@@ -148,3 +148,21 @@ def test_rows_past_32_bits_of_offset():
     y = i8.cfint8_dequantize(q, s, rows, cols, dtype=torch.bfloat16)
     torch.cuda.synchronize()
     R.same_bits(y[pick], torch.from_numpy(wq.astype(np.float32) * ws[:, None]).to(torch.bfloat16), "values")
+
+
+@pytest.mark.parametrize("axis", [1, 0])
+def test_more_lines_than_a_launch_takes(axis):
+    lines, k = (1 << 21) + 37, 5
+    say(f"[int8 quantize] {lines} lines, axis {axis}")
+    rng = np.random.default_rng(3)
+    v = rng.standard_normal((lines, k)).astype(np.float32)
+    if axis == 1:
+        x = torch.zeros((lines, 8), device=R.DEV)[:, :k]
+        x.copy_(torch.from_numpy(v))
+    else:
+        x = torch.from_numpy(np.ascontiguousarray(v.T)).to(R.DEV)
+    q, s = i8.cfint8_quantize(x, block_axis=axis)
+    wq, ws = R.quantize(v)
+    assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws)
+    y = i8.cfint8_dequantize(q, s, lines, k)
+    R.same_bits(y, torch.from_numpy(wq.astype(np.float32) * ws[:, None]), "values")
