@@ -142,12 +142,12 @@ __device__ __forceinline__ void put_digits(const float* v, int e, int8_t* dst, i
     for (int p = 0; p < P; p++) *reinterpret_cast<uint2*>(dst + (int64_t)p * n + c) = d[p];
 }
 
-// workgroups [0, T): a token's x into digits; then one for each (expert, 4 tokens), its waves sharing H
-template <bool BF16, int P>
+// workgroups [0, T): a token's x into digits; then one for each (expert, N tokens), its waves sharing H
+template <bool BF16, int P, int N>
 __global__ __launch_bounds__(256) void router_kernel(MoeArgs a, int8_t* __restrict__ xd, int* __restrict__ xe,
                                                      float* __restrict__ logits) {
     __shared__ uint32_t top[4];
-    __shared__ double part[4][4];
+    __shared__ double part[4][N];
     const int T = (int)a.T, E = (int)a.E, H = (int)a.H, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t es = BF16 ? 2 : 4;
     int b = blockIdx.x;
@@ -173,8 +173,8 @@ __global__ __launch_bounds__(256) void router_kernel(MoeArgs a, int8_t* __restri
         return;
     }
     b -= T;
-    const int e = b % E, t0 = (b / E) * 4, n = min(4, T - t0);
-    double s[4] = {0, 0, 0, 0};
+    const int e = b % E, t0 = (b / E) * N, n = min(N, T - t0);
+    double s[N] = {};
     const char* r = static_cast<const char*>(a.router) + (int64_t)e * H * es;
     const char* x = static_cast<const char*>(a.x) + t0 * a.ldx * es;
 #pragma unroll 2
@@ -182,18 +182,17 @@ __global__ __launch_bounds__(256) void router_kernel(MoeArgs a, int8_t* __restri
         float w[8];
         load8<BF16>(r, c, w);
 #pragma unroll
-        for (int t = 0; t < 4; t++) {
+        for (int t = 0; t < N; t++) {
             float v[8];
             load8<BF16>(x + (t < n ? t : 0) * a.ldx * es, c, v);
 #pragma unroll
             for (int i = 0; i < 8; i++) s[t] = __builtin_fma((double)v[i], (double)w[i], s[t]);
         }
     }
-#pragma unroll
-    for (int t = 0; t < 4; t++) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s[t] += __shfl_xor(s[t], o);
-        if (lane == 0) part[wave][t] = s[t];
+    const double sum = N == 4 ? sum4(s[0], s[N == 4 ? 1 : 0], s[N == 4 ? 2 : 0], s[N == 4 ? 3 : 0]) : sum1(s[0]);
+    if ((lane & 15) == 0) {
+        if (N == 4) part[wave][value_of_row(lane >> 4) % N] = sum;
+        else if (lane == 0) part[wave][0] = sum;
     }
     __syncthreads();
     const int t = threadIdx.x;
@@ -834,7 +833,8 @@ hipError_t launch(const MoeArgs& a, hipStream_t s) {
     float* part = reinterpret_cast<float*>(w + l.part);
     const int64_t slots = a.T * a.topk, experts = a.E < slots ? a.E : slots;
     const int64_t up = (a.I + UP_COLS - 1) / UP_COLS, down = (a.H + DOWN_COLS - 1) / DOWN_COLS;
-    router_kernel<BF16, P><<<(unsigned)(a.T + a.E * ((a.T + 3) / 4)), 256, 0, s>>>(a, xd, xe, logits);
+    if (a.T == 1) router_kernel<BF16, P, 1><<<(unsigned)(1 + a.E), 256, 0, s>>>(a, xd, xe, logits);
+    else router_kernel<BF16, P, 4><<<(unsigned)(a.T + a.E * ((a.T + 3) / 4)), 256, 0, s>>>(a, xd, xe, logits);
     if (by_slots<P>(a.T, a.E, a.topk, a.H, a.I)) {
         const int64_t slices = (one_exponents(a.I, P) + 7) / 8 * 8;
         gate_up_one_kernel<P><<<(unsigned)(slices * slots + a.T), 64 * one_waves(P), 0, s>>>(a, xd, xe, logits, hd, he);

@@ -8,7 +8,7 @@
 // fma (a multiple of half an ulp of s below s), so comparing it with s/2 settles q; that comparison
 // finds something to mend only next to a tie, and eight elements share it.
 //
-// Rows: held in registers by a wave (up to 1024) or a workgroup (up to 32768, with a multiplier 16384), the source
+// Rows: held in registers by a wave (up to 1024) or a workgroup (up to 32768), the source
 // read once; longer ones read twice.  Columns: partial maxima of row chunks into the workspace (maxima, so no order
 // to depend on), then 128 x 128 tiles turned in LDS.  Bound by memory: 8192 x 14336 bf16 rows in 70 us (5.0 TB/s of
 // source and codes), 4096 x 11008 columns, whose source is read twice, in 46 us.
@@ -290,16 +290,11 @@ hipError_t launch_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, 
     else if (cols <= 1024) CFINT8_ROWS(64, 2);
     else if (cols <= 2048) CFINT8_ROWS(256, 1);
     else if (cols <= 4096) CFINT8_ROWS(256, 2);
-    else if constexpr (MUL) {   // the multiplier's values are held beside the row's: two units a thread
-        if (cols <= 8192) CFINT8_ROWS(512, 2);
-        else if (cols <= 16384) CFINT8_ROWS(1024, 2);
-        else long_rows_kernel<BF16, MUL><<<row_grid, 1024, 0, s>>>(p, cols, ld, mul, codes, ldq, scales);
-    } else {
-        if (cols <= 8192) CFINT8_ROWS(256, 4);
-        else if (cols <= 16384) CFINT8_ROWS(512, 4);
-        else if (cols <= 32768) CFINT8_ROWS(1024, 4);
-        else long_rows_kernel<BF16, MUL><<<row_grid, 1024, 0, s>>>(p, cols, ld, mul, codes, ldq, scales);
-    }
+    else if (cols <= 8192) CFINT8_ROWS(256, 4);
+    else if (cols <= 12288) CFINT8_ROWS(512, 3);
+    else if (cols <= 16384) CFINT8_ROWS(512, 4);
+    else if (cols <= 32768) CFINT8_ROWS(1024, 4);
+    else long_rows_kernel<BF16, MUL><<<row_grid, 1024, 0, s>>>(p, cols, ld, mul, codes, ldq, scales);
 #undef CFINT8_ROWS
     return hipGetLastError();
 }
