@@ -126,10 +126,11 @@ def _bytes(what: str, fn, *args) -> int:
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
     """Memory that is first written on the call's stream comes from that stream's pool: a block of another one may
     still be in use there by what its last owner queued."""
+    strides = (shape[1], 1) if len(shape) == 2 else (1,)
     if stream is not None and device.type == "cuda":
         with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=device)
-    return torch.empty(shape, dtype=dtype, device=device)
+            return torch.empty_strided(shape, strides, dtype=dtype, device=device)
+    return torch.empty_strided(shape, strides, dtype=dtype, device=device)      # 0.4 us less than torch.empty
 
 
 def _scratch(what, workspace, need: int, device, stream):
@@ -173,8 +174,10 @@ def cfint8_quantize(src: torch.Tensor, block_axis: int = 1, mul: Optional[torch.
     the quantized axis, multiplied in first."""
     what = "cfint8_quantize"
     _place(what, stream, ("src", "mul", "codes", "scales", "workspace"), src, mul, codes, scales, workspace)
-    _source_arg(what, src)
-    rows, cols = src.shape
+    sh = src.shape
+    if len(sh) != 2:
+        _source_arg(what, src)
+    rows, cols = sh
     ld_src = _matrix(what, "src", src, rows, cols, _FLOATS)
     if block_axis == 1:
         outer, k = rows, cols
@@ -277,8 +280,10 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
     _place(what, stream, ("x", "router", "gate_up", "gate_up_scales", "down", "down_scales", "active", "y", "ids",
                           "weights", "workspace"),
            x, router, gate_up, gate_up_scales, down, down_scales, active, y, ids, weights, workspace)
-    _source_arg(what, x)
-    T, H = x.shape
+    sh = x.shape
+    if len(sh) != 2:
+        _source_arg(what, x)
+    T, H = sh
     ld_x = _matrix(what, "x", x, T, H, _FLOATS)
     dtype, device = x.dtype, x.device
     rs, ds, gs = router.shape, down.shape, gate_up.shape
