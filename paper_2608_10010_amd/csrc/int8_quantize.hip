@@ -10,7 +10,7 @@
 //
 // Rows: held in registers by a wave (up to 1024) or a workgroup (up to 32768), the source
 // read once; longer ones read twice.  Columns: partial maxima of row chunks into the workspace (maxima, so no order
-// to depend on), then 128 x 128 tiles turned in LDS.  Bound by memory: 8192 x 14336 bf16 rows in 70 us (5.0 TB/s of
+// to depend on), then 128 x 128 tiles turned in LDS; up to 256 rows all at once.  Bound by memory: 8192 x 14336 bf16 rows in 70 us (5.0 TB/s of
 // source and codes), 4096 x 11008 columns, whose source is read twice, in 46 us.
 #include <type_traits>
 
@@ -138,13 +138,13 @@ __device__ __forceinline__ void mask8(float* v, I c, I n) {
     }
 }
 
-// eight elements of a row for the column kernels: whole ones, or element by element where the row's pieces are not aligned
-// or end (columns past the last repeat it)
-template <bool BF16, bool WHOLE, bool LAST>
+// Eight elements of a row for the column kernels, by pieces (past the last whole eight these again) or, where the row's
+// pieces are not aligned or end among the eight, element by element (past the last it again)
+template <bool BF16, bool PIECES, bool LAST>
 __device__ __forceinline__ Raw<BF16> load_columns(const char* p, int64_t c, int64_t n) {
     Raw<BF16> r;
-    if (WHOLE) {
-        const uint4* q = reinterpret_cast<const uint4*>(p + c * (BF16 ? 2 : 4));
+    if (PIECES) {
+        const uint4* q = reinterpret_cast<const uint4*>(p + min(c, n / 8 * 8 - 8) * (BF16 ? 2 : 4));
         r.a = ld16<LAST>(q);
         if (!BF16) r.b = ld16<LAST>(q + 1);
         return r;
@@ -325,16 +325,21 @@ __global__ __launch_bounds__(256) void col_max_kernel(const char* __restrict__ s
     uint32_t m[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) m[i] = 0;
-    auto scan = [&](auto whole) {
+    const bool ends = c < cols && c + 8 > cols;   // the row ends among this thread's columns
+    auto scan = [&](auto pieces) {
         for (int64_t r = r0 + rl; r < r1; r += 16 * BATCH) {
             Raw<BF16> raw[BATCH];
             float f[BATCH];
 #pragma unroll
             for (int u = 0; u < BATCH; u++) {
                 const int64_t at = min(r + 16 * u, r1 - 1);
-                raw[u] = load_columns<BF16, decltype(whole)::value, false>(src + at * ld * (BF16 ? 2 : 4), c, cols);
+                raw[u] = load_columns<BF16, decltype(pieces)::value, false>(src + at * ld * (BF16 ? 2 : 4), c, cols);
                 f[u] = MUL ? mul[at] : 1.f;
             }
+            if (decltype(pieces)::value && ends)
+#pragma unroll
+                for (int u = 0; u < BATCH; u++)
+                    raw[u] = load_columns<BF16, false, false>(src + min(r + 16 * u, r1 - 1) * ld * (BF16 ? 2 : 4), c, cols);
 #pragma unroll
             for (int u = 0; u < BATCH; u++) {
                 float v[8];
@@ -344,7 +349,7 @@ __global__ __launch_bounds__(256) void col_max_kernel(const char* __restrict__ s
             }
         }
     };
-    if (ALIGNED && c0 + TILE <= cols) scan(std::true_type{});
+    if (ALIGNED && cols >= 8) scan(std::true_type{});
     else scan(std::false_type{});
 #pragma unroll
     for (int i = 0; i < 8; i++) red[rl][cl * 8 + i] = m[i];
@@ -362,18 +367,21 @@ __global__ __launch_bounds__(256) void col_max_kernel(const char* __restrict__ s
 // one column go to LDS (16-byte pieces of a column's 128 bytes XOR-swizzled by the column's group of 8, so that the
 // 16 lanes of a row segment spread over the banks), and leave as 16-byte pieces of code rows.  (Turning the values in
 // LDS before they are quantized takes 53 KB, so three workgroups a unit: 37 us against 29 on 4096 x 11008 bf16.)
-template <bool BF16, bool MUL, bool ALIGNED>
-__global__ __launch_bounds__(256) void cols_kernel(const char* __restrict__ src, int64_t rows, int64_t cols, int64_t ld,
+// ONCE > 0: up to 128 ONCE rows in one launch, 256 threads for each 128 of them, which find the columns' maxima in LDS.
+template <bool BF16, bool MUL, bool ALIGNED, int ONCE>
+__global__ __launch_bounds__(ONCE > 0 ? 256 * ONCE : 256) void cols_kernel(const char* __restrict__ src, int64_t rows, int64_t cols, int64_t ld,
                                                    const float* __restrict__ mul, const uint32_t* __restrict__ partial,
                                                    int chunks, int8_t* __restrict__ codes, int64_t ldq,
                                                    float* __restrict__ scales) {
-    __shared__ uint32_t top[2][TILE];
+    constexpr int TILES = ONCE > 0 ? ONCE : 1;
+    __shared__ uint32_t top[ONCE > 0 ? 4 * ONCE : 2][TILE];
     __shared__ __attribute__((aligned(16))) float4 line[TILE];   // s, 1 / s, pre, zero
-    __shared__ __attribute__((aligned(16))) uint32_t tile[TILE * TILE / 4];
-    const int tid = threadIdx.x;
-    const int64_t c0 = (int64_t)blockIdx.x * TILE, r0 = (int64_t)blockIdx.y * TILE;
+    __shared__ __attribute__((aligned(16))) uint32_t tiles[TILES][TILE * TILE / 4];
+    const int tid = threadIdx.x & 255, block = ONCE > 0 ? threadIdx.x >> 8 : (int)blockIdx.y;
+    uint32_t* tile = tiles[ONCE > 0 ? block : 0];
+    const int64_t c0 = (int64_t)blockIdx.x * TILE, r0 = (int64_t)block * TILE;
     uint32_t part[MAX_CHUNKS / 2];   // every other chunk; past the last one it again
-    {
+    if (ONCE == 0) {
         const int64_t col = min(c0 + (tid & 127), cols - 1);
 #pragma unroll
         for (int k = 0; k < MAX_CHUNKS / 2; k++)
@@ -383,17 +391,33 @@ __global__ __launch_bounds__(256) void cols_kernel(const char* __restrict__ src,
     const int64_t c = c0 + cl * 8;
     Raw<BF16> raw[8];
     float f[8];
-    auto load = [&](auto whole) {
+    auto load = [&](auto pieces) {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const int64_t r = min(r0 + (i >> 2) * 64 + rl * 4 + (i & 3), rows - 1);
-            raw[i] = load_columns<BF16, decltype(whole)::value, true>(src + r * ld * (BF16 ? 2 : 4), c, cols);
+            raw[i] = load_columns<BF16, decltype(pieces)::value, true>(src + r * ld * (BF16 ? 2 : 4), c, cols);
             f[i] = MUL ? mul[r] : 1.f;
         }
     };
-    if (ALIGNED && c0 + TILE <= cols) load(std::true_type{});
-    else load(std::false_type{});
-    {
+    if (!ALIGNED || cols < 8) load(std::false_type{});
+    else load(std::true_type{});
+    if (ALIGNED && cols >= 8 && c < cols && c + 8 > cols) load(std::false_type{});   // the row ends among these eight
+    if (ONCE > 0) {   // rows past the last one repeat it
+        uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            float x[8];
+            raw[i].unpack(x);
+#pragma unroll
+            for (int j = 0; j < 8; j++) m[j] = max(m[j], __float_as_uint(MUL ? x[j] * f[i] : x[j]) & 0x7FFFFFFFu);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) {   // over the wave's four row groups
+            m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 16));
+            m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 32));
+            if ((tid & 63) < 16) top[threadIdx.x >> 6][cl * 8 + j] = m[j];
+        }
+    } else {
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < MAX_CHUNKS / 2; k++)
@@ -401,10 +425,13 @@ __global__ __launch_bounds__(256) void cols_kernel(const char* __restrict__ src,
         top[tid >> 7][tid & 127] = m;
     }
     __syncthreads();
-    if (tid < TILE) {
-        const Line l = make_line(max(top[0][tid], top[1][tid]));
+    if (threadIdx.x < TILE) {
+        uint32_t m = top[0][tid];
+#pragma unroll
+        for (int k = 1; k < (ONCE > 0 ? 4 * ONCE : 2); k++) m = max(m, top[k][tid]);
+        const Line l = make_line(m);
         line[tid] = make_float4(l.s, l.inv, l.pre, l.zero ? 1.f : 0.f);
-        if (blockIdx.y == 0 && c0 + tid < cols) scales[c0 + tid] = l.out;
+        if (r0 == 0 && c0 + tid < cols) scales[c0 + tid] = l.out;
     }
     float v[2][4][8];
 #pragma unroll
@@ -456,11 +483,20 @@ hipError_t launch_cols(const void* src, int64_t rows, int64_t cols, int64_t ld, 
     uint32_t* partial = static_cast<uint32_t*>(ws);
     const int64_t chunks = col_chunks(rows, cols), chunk_rows = (rows + chunks - 1) / chunks;
     const unsigned ct = (unsigned)((cols + TILE - 1) / TILE);
+    // few rows: one launch, the source read once (64 x 4096 bf16 9.0 -> 6.6 us, 200 x 14336 fp32 10.2 -> 8.3; with 512 rows
+    // in a workgroup 512 x 14336 fp32 takes 14.4 instead of 11.8)
+    if (rows <= 2 * TILE) {
+        if (rows <= TILE)
+            cols_kernel<BF16, MUL, ALIGNED, 1><<<ct, 256, 0, s>>>(p, rows, cols, ld, mul, nullptr, 0, codes, ldq, scales);
+        else
+            cols_kernel<BF16, MUL, ALIGNED, 2><<<ct, 512, 0, s>>>(p, rows, cols, ld, mul, nullptr, 0, codes, ldq, scales);
+        return hipGetLastError();
+    }
     col_max_kernel<BF16, MUL, ALIGNED><<<dim3(ct, (unsigned)chunks), 256, 0, s>>>(p, rows, cols, ld, mul, chunk_rows,
                                                                                 partial);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    cols_kernel<BF16, MUL, ALIGNED><<<dim3(ct, (unsigned)((rows + TILE - 1) / TILE)), 256, 0, s>>>(
+    cols_kernel<BF16, MUL, ALIGNED, 0><<<dim3(ct, (unsigned)((rows + TILE - 1) / TILE)), 256, 0, s>>>(
         p, rows, cols, ld, mul, partial, (int)chunks, codes, ldq, scales);
     return hipGetLastError();
 }

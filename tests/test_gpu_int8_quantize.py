@@ -166,3 +166,14 @@ def test_more_lines_than_a_launch_takes(axis):
     assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws)
     y = i8.cfint8_dequantize(q, s, lines, k)
     R.same_bits(y, torch.from_numpy(wq.astype(np.float32) * ws[:, None]), "values")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(128, 7), (256, 8), (255, 9), (257, 1030), (200, 127), (129, 129), (300, 1), (400, 135)])
+def test_columns_that_end_inside_pieces(rows, cols, dtype):
+    """Rows whose pieces are aligned (a wider buffer) and not, in one launch and in two."""
+    rng = np.random.default_rng(rows * cols)
+    m = np.exp(rng.standard_normal(rows)).astype(np.float32)
+    say(f"[int8 quantize] columns {rows} x {cols} {dtype}")
+    for pad in (0, -cols % 8, 1):
+        check(source(rng, rows, cols, dtype), dtype, 0, m if pad else None, pad=pad, ldq=R.ceil16(rows) + 16)
