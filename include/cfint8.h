@@ -107,6 +107,8 @@ int cfint8_gemm(const int8_t* a, int64_t lda, const float* a_scales, const int8_
  *   y        [T][ld_y] of `dtype`, 16-byte aligned rows; ids int32 and weights fp32 [T][topk].
  *   workspace  at least cfint8_moe_workspace_bytes bytes, 256-byte aligned; scratch, so calls that share it must be
  *            ordered.
+ * Values leave fp32's range where g, u, h, a slot's (h . down) s or y do, not where a sum of codes does that its scale
+ * brings back.
  * A NaN or an infinity in x gives NaN in that token's y (in no other's).
  * Errors: CURVEFP_ERR_NULL, _FORMAT (dtype), _SHAPE, _ALIGN, _HIP.
  */

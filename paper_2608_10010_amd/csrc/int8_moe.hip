@@ -437,11 +437,18 @@ __device__ __forceinline__ void shared_sum(const char* ring0, int half, int t, i
     out[0] = s.x, out[1] = s.y, out[2] = s.z, out[3] = s.w;
 }
 
-// f 2^e; NaN where e says so
-__device__ __forceinline__ float scaled_by(float f, int e) {
-    return e == POISON ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(f, e);
+// A scale's significand multiplies where its exponent was added before, so that only g, u and y can leave fp32's range,
+// not a sum that its scale would have brought back
+__device__ __forceinline__ int exponent_of(float s) { return __builtin_amdgcn_frexp_expf(s); }
+__device__ __forceinline__ float significand_of(float s) { return __builtin_amdgcn_frexp_mantf(s); }
+
+// f 2^(e + more); NaN where e says so
+__device__ __forceinline__ float scaled_by(float f, int e, int more) {
+    return e == POISON ? __uint_as_float(0x7FC00000u) : __builtin_amdgcn_ldexpf(f, e + more);
 }
-__device__ __forceinline__ float row_scaled(float f, int e, float s) { return scaled_by(f, e) * s; }
+__device__ __forceinline__ float row_scaled(float f, int e, float s) {
+    return scaled_by(f * significand_of(s), e, exponent_of(s));
+}
 
 // Waves of even number take the first 32 columns, the others the last
 template <int P>
@@ -564,7 +571,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
         const int col = threadIdx.x % DOWN_COLS, c = c0 + col;
         int slot[ROUNDS][4];
         float weight[ROUNDS][4];
-        const float sd = c < H ? a.dns[(int64_t)e * H + c] : 0.f;
+        const float sd = a.dns[(int64_t)e * H + min(c, H - 1)];   // past the last column it again
 #pragma unroll
         for (int i = 0; i < ROUNDS; i++)
 #pragma unroll
@@ -573,6 +580,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
                 weight[i][v] = a.weights[slot[i][v]];
             }
         float f[NT][4] = {};
+        float sc[NT];   // of this lane's columns, for their exponents, which wait for them behind the first codes' request
+#pragma unroll
+        for (int t = 0; t < NT; t++) sc[t] = a.dns[(int64_t)e * H + min(c0 + 64 * half + 16 * t + (lane & 15), H - 1)];
         stream<P, NT, WAVES / 2, true>(
             hd, slots * P * I, r < n ? rows[r] * P * I : NONE, he, 2 * slots * row_exps, exp_offset, b, I, wave >> 1, ring0,
             ring1, [&](const i32x4(&fa)[P], const i32x4(&fb)[NT], const int(&ex)[4]) __attribute__((always_inline)) {
@@ -586,7 +596,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
 #pragma unroll
                 for (int t = 0; t < NT; t++)
 #pragma unroll
-                    for (int v = 0; v < 4; v++) f[t][v] += scaled_by(join<P, NT>(acc, t, v), ex[v]);
+                    for (int v = 0; v < 4; v++) f[t][v] += scaled_by(join<P, NT>(acc, t, v), ex[v], exponent_of(sc[t]));
             });
         share_sums<NT>(f, ring0);
 #pragma unroll
@@ -598,7 +608,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void down_kernel(MoeArgs a, const in
 #pragma unroll
             for (int v = 0; v < 4; v++) {
                 if (r0 + 4 * q + v >= n) break;
-                const float y = s[v] * sd * weight[i][v];
+                const float y = s[v] * significand_of(sd) * weight[i][v];
                 part[(int64_t)slot[i][v] * H + c] = y;
             }
         }
@@ -784,14 +794,16 @@ __global__ __launch_bounds__(512) void down_one_kernel(MoeArgs a, const int8_t* 
             const float* sd = a.dns + (int64_t)e * H + c0 + col;
             const float s0 = sd[0], s1 = sd[4], weight = a.weights[slot];
             __builtin_amdgcn_sched_barrier(0);
+            const int e0 = exponent_of(s0), e1 = exponent_of(s1);
             float f[COLS];
 #pragma unroll
             for (int r = 0; r < COLS; r++) {
                 int acc[P] = {};
                 dots<P>(d, v[r], acc);
-                f[r] = scaled_by(join1<P>(acc), ex);
+                f[r] = scaled_by(join1<P>(acc), ex, __builtin_amdgcn_readlane(r < 4 ? e0 : e1, 16 * value_of_row(r & 3)));
             }
-            const float y0 = sum4(f[0], f[1], f[2], f[3]) * s0 * weight, y1 = sum4(f[4], f[5], f[6], f[7]) * s1 * weight;
+            const float y0 = sum4(f[0], f[1], f[2], f[3]) * significand_of(s0) * weight;
+            const float y1 = sum4(f[4], f[5], f[6], f[7]) * significand_of(s1) * weight;
             if ((lane & 15) == 0) part[it][col] = y0, part[it][4 + col] = y1;
         }
     __syncthreads();
