@@ -303,6 +303,8 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
     _vector(what, "down_scales", down_scales, E * H)
     if active is not None:
         _vector(what, "active", active, T, torch.bool if active.dtype == torch.bool else torch.uint8)
+    L = lib()
+    need = _bytes(what, L.cfint8_moe_workspace_bytes, T, E, topk, H, I)     # refuses sizes before anything is allocated
     if y is None:
         y = _empty((T, H), dtype, device, stream)
     ld_y = _matrix(what, "y", y, T, H, (dtype,))
@@ -314,9 +316,7 @@ def cfint8_moe(x: torch.Tensor, router: torch.Tensor, gate_up: torch.Tensor, gat
         weights = _empty((T, topk), torch.float32, device, stream)
     else:
         _vector(what, "weights", weights, T * topk)
-    L = lib()
-    wp, wb, held = _scratch(what, workspace, _bytes(what, L.cfint8_moe_workspace_bytes, T, E, topk, H, I), device,
-                            stream)
+    wp, wb, held = _scratch(what, workspace, need, device, stream)
     st = L.cfint8_moe(x.data_ptr(), DTYPES[dtype], T, H, ld_x, router.data_ptr(), E, gate_up.data_ptr(),
                       gate_up_scales.data_ptr(), down.data_ptr(), down_scales.data_ptr(), I, topk,
                       1 if renormalize else 0, _ptr(active), y.data_ptr(), ld_y, ids.data_ptr(),

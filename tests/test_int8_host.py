@@ -254,3 +254,13 @@ def test_binding_moe(meta):
         call(topk=9)
     with pytest.raises(cf.CurveFPError):
         call(x=(300, 64))
+
+
+@pytest.mark.parametrize("topk", [-1, 0, 9, 33, 1 << 40])
+def test_binding_moe_refuses_topk_before_it_allocates(meta, topk):
+    """The library's error, whatever ids and weights of that size would have done."""
+    f32 = torch.float32
+    with pytest.raises(cf.CurveFPError) as e:
+        i8.cfint8_moe(meta((4, 64), f32), meta((8, 64), f32), meta((8, 64, 64)), meta((8, 64), f32), meta((8, 64, 32)),
+                      meta((8, 64), f32), topk, stream=STREAM)
+    assert e.value.status == ESHAPE
