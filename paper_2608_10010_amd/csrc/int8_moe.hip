@@ -20,6 +20,7 @@
 #include "../../include/cfint8.h"
 #include "int8_internal.hpp"
 #include "int8_lanes.hpp"
+#include "int8_routes.hpp"
 
 namespace cfint8 {
 
@@ -29,8 +30,6 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int POISON = INT16_MIN;      // exponent of values among which is a NaN or an infinity
 constexpr int ROWS = 16;               // token rows of a matrix product
-constexpr int64_t UNITS = 256;         // compute units
-constexpr int RANKED_EXPERTS = 256;    // experts among which gate_up_one ranks
 constexpr int UP_COLS = 64;            // inner columns of a gate_up workgroup: h's columns of one exponent
 constexpr int DOWN_COLS = 128;         // output columns of a down workgroup
 constexpr int WAVES = 4;               // of either
@@ -814,24 +813,6 @@ __global__ __launch_bounds__(512) void down_one_kernel(MoeArgs a, const int8_t* 
     const int64_t at = t * a.ldy + c0 + threadIdx.x;
     if (BF16) static_cast<uint16_t*>(a.y)[at] = (uint16_t)to_bf16(s);
     else static_cast<float*>(a.y)[at] = s;
-}
-
-// Slot by slot or expert by expert, by estimated time in us: three launches and their latencies, the weights of the
-// experts that T tokens take on average at 5.4 TB/s and those that slots share at 6.5, or 6 us for each 512
-// workgroups, which rank E logits first; or five launches and the experts' weights at 5.2 TB/s (fp32: 4.6).  (1 token, 8
-// of 64 experts of 2048 x 1024: 18 us against 40; 4 tokens 46 against 52; 12 tokens, 4 of 128 60 against 74; 16 tokens, 8
-// of 128 of 2048 x 768 107 against 102; 64 tokens, 2 of 16 103 against 45; fp32, 7 tokens, 2 of 16 of 4096 x 2048 68
-// against 77.)
-template <int P>
-bool by_slots(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I) {
-    if (E > RANKED_EXPERTS) return false;
-    const double weights = 3e-6 * (double)H * (double)I, slots = (double)(T * k);   // 1 MB takes 1 us at 1 TB/s
-    const double rounds = slots * (double)((I + 31) / 32) / (2.0 * UNITS), chunks = (double)((E + 63) / 64);
-    double untaken = 1;
-    for (int64_t t = 0; t < T; t++) untaken *= 1 - (double)k / (double)E;
-    const double taken = (double)E * (1 - untaken);
-    const double read = taken * weights / 5.4 + (slots - taken) * weights / 6.5;
-    return 10 + (read > 6 * rounds ? read : 6 * rounds) + 0.6 * rounds * chunks * chunks < 25 + taken * weights / (P == 4 ? 4.6 : 5.2);
 }
 
 template <bool BF16, int P>
