@@ -177,3 +177,25 @@ def test_columns_that_end_inside_pieces(rows, cols, dtype):
     say(f"[int8 quantize] columns {rows} x {cols} {dtype}")
     for pad in (0, -cols % 8, 1):
         check(source(rng, rows, cols, dtype), dtype, 0, m if pad else None, pad=pad, ldq=R.ceil16(rows) + 16)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [3000, 5900, 6143, 6144, 6145, 6151, 8193, 11007, 12287, 12288, 12289, 12295, 24001])
+def test_rows_of_three_units_a_thread(cols, dtype):
+    """Both ends of the row kernels with three units a thread (to 6144 and to 12288) and inside their third."""
+    rng = np.random.default_rng(cols)
+    for rows, mul in ((3, True), (2, False)):
+        say(f"[int8 quantize] rows={rows} cols={cols} {dtype} mul={mul}")
+        m = np.exp(rng.standard_normal(cols)).astype(np.float32) if mul else None
+        check(source(rng, rows, cols, dtype), dtype, 1, m, pad=-cols % 8 + 8, ldq=R.ceil16(cols) + 32)
+
+
+@pytest.mark.parametrize("axis", [0, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(3, 5001), (2, 11111), (2, 20004), (2, 33001), (200, 136), (300, 136)])
+def test_borders_in_every_kernel(rows, cols, dtype, axis):
+    """Quotients next to ties, and lines whose scale is subnormal or rounds to 0, past the narrowest kernels."""
+    rng = np.random.default_rng(cols)
+    for kind in ("halves", "tiny", "huge"):
+        say(f"[int8 quantize] {kind} {dtype} axis={axis} {rows}x{cols}")
+        check(source(rng, rows, cols, dtype, kind), dtype, axis, pad=-cols % 8)
