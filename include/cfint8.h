@@ -34,7 +34,7 @@ extern "C" {
  *         for a gradient whose product contracts over the axis that another operand's scales lie on);
  *   s   = max |v_k| / 127, rounded to fp32;
  *   q_k = v_k / s (the exact quotient) rounded to the nearest integer, ties to even.
- * A line of zeros has s = 0 and zero codes.  A line that holds a NaN or an infinity (in v) has s = NaN
+ * A line whose s is 0 (of zeros, or of values so small that s rounds to 0) has zero codes.  A line that holds a NaN or an infinity (in v) has s = NaN
  * and zero codes.  Where s is subnormal (max |v| below about 1.5e-36) codes are clamped to +-127.
  *   src     [rows][ld_src] of `dtype` (fp32 or bf16).  block_axis = 1: 16-byte aligned rows, each readable
  *           up to the next multiple of 16 bytes; block_axis = 0: element alignment suffices.

@@ -8,9 +8,10 @@
 // codes are swizzled, so that the fragment reads cover all banks.  A block's second half is read under the first
 // half's MFMAs, the next block's first half and the copy of a later block go out under the second half's.  A
 // 256 x 256 tile needs 192 KB through the LDS a block (reads and copies) for 2048 cycles of MFMA, 75% of its rate;
-// smaller wave tiles would need more of it than there is.  At 8192 x 14336 x 4096 (437 us, 2200 TOPS) the matrix pipe
-// is busy for 74% of the cycles of a clock that the power limit holds at 1.67 GHz.  C goes past the caches that A and B
-// are read from (streaming stores: 415 us; no size measured loses more than 3%).
+// smaller wave tiles would need more of it than there is.  At 8192 x 14336 x 4096 (420 us, 2290 TOPS; 430
+// to 480 where calls follow each other without a wait) the matrix pipe is busy for 64% of a unit's cycles, at a clock that the
+// power limit holds at 1.8 GHz.  C goes past the caches that A and B are read from (streaming stores: 434 -> 415 us; no
+// size measured loses more than 3%).
 //
 // An operand that lies as [K][N] goes to LDS in its own order and is turned by transposing reads on its way to
 // registers (4096 x 4096 x 14336 210 us against 235 with a pass that turns it first, 2048 x 2048 x 2048 14.6 against 21).

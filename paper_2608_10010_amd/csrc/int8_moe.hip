@@ -4,7 +4,9 @@
 // memory, and the codes go from memory to the matrix cores as they are.  The other operand of
 // v_mfma_i32_16x16x64_i8 is the activation in fixed point: a row's values as integers of 22 bits (bf16) or
 // 30 bits (fp32) below a power of two above its largest, split into 3 or 4 signed base-256 digits, one
-// product for each digit.  All sums of products are exact int32; the digits' sums meet in fp32.
+// product for each digit.  All sums of products are exact int32; the digits' sums meet in fp32.  What lies 2^23 below a
+// row's largest is lost to bf16 calls, whose results are rounded to 2^-9: a fourth digit there takes 64 tokens over 128
+// experts from 164 to 173 us, one token from 17.2 to 18.5, 8 tokens over 88 experts from 24.5 to 34.8.
 //
 //   router   logits in 64 bits (they decide, so they are right to the last bit); x into digits
 // and, where the tokens' experts are mostly different ones (one token above all),

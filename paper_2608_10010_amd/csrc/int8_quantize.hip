@@ -10,8 +10,9 @@
 //
 // Rows: held in registers by a wave (up to 1024) or a workgroup (up to 32768), the source
 // read once; longer ones read twice.  Columns: partial maxima of row chunks into the workspace (maxima, so no order
-// to depend on), then 128 x 128 tiles turned in LDS; up to 256 rows all at once.  Bound by memory: 8192 x 14336 bf16 rows in 70 us (5.0 TB/s of
-// source and codes), 4096 x 11008 columns, whose source is read twice, in 46 us.
+// to depend on), then 128 x 128 tiles turned in LDS; up to 256 rows all at once.  Bound by memory: 8192 x 14336 bf16 rows
+// in 57 to 64 us (5.5 to 6.2 TB/s of source and codes; vector instructions take 93% of a busy unit's issue slots, so not much
+// more would fit), 4096 x 11008 columns, whose source is read twice, in 42.
 #include <type_traits>
 
 #include "device_util.hpp"
@@ -307,7 +308,7 @@ constexpr int TILE = 128;         // columns and rows of a tile
 constexpr int MAX_CHUNKS = 32;    // row chunks with a partial maximum of their own
 
 // As many as give col_max 1024 workgroups, of at least 64 rows: every tile reads all of its columns' partial maxima
-// (4096 x 11008 bf16: 12 chunks 46 us, 32 chunks 48 us)
+// (2048 x 14336 bf16: 10 chunks 28.8 us, 32 chunks 30.7 us; 4096 x 11008: 12 and 32 alike)
 int64_t col_chunks(int64_t rows, int64_t cols) {
     const int64_t tiles = (cols + TILE - 1) / TILE, want = (1024 + tiles - 1) / tiles, most = (rows + 63) / 64;
     const int64_t n = want < most ? want : most;
@@ -368,7 +369,8 @@ __global__ __launch_bounds__(256) void col_max_kernel(const char* __restrict__ s
 // A tile of 128 rows x 128 columns: a thread quantizes 4 rows x 8 columns twice from its registers, words of 4 codes of
 // one column go to LDS (16-byte pieces of a column's 128 bytes XOR-swizzled by the column's group of 8, so that the
 // 16 lanes of a row segment spread over the banks), and leave as 16-byte pieces of code rows.  (Turning the values in
-// LDS before they are quantized takes 53 KB, so three workgroups a unit: 37 us against 29 on 4096 x 11008 bf16.)
+// LDS before they are quantized takes 53 KB, so three workgroups a unit: 37 us on 4096 x 11008 bf16, this form 29 then
+// and 24 now.)
 // ONCE > 0: up to 128 ONCE rows in one launch, 256 threads for each 128 of them, which find the columns' maxima in LDS.
 template <bool BF16, bool MUL, bool ALIGNED, int ONCE>
 __global__ __launch_bounds__(ONCE > 0 ? 256 * ONCE : 256) void cols_kernel(const char* __restrict__ src, int64_t rows, int64_t cols, int64_t ld,
@@ -507,7 +509,7 @@ hipError_t launch_cols(const void* src, int64_t rows, int64_t cols, int64_t ld, 
 
 // four codes a thread and round; a workgroup takes `per` whole rows (rows of up to 2048) or a segment of 4096 of
 // one.  A thread requests its four rounds before it writes the first, by streaming stores: 8192 x 14336 to fp32
-// 144 -> 84 us (7.0 TB/s)
+// 144 -> 85 us (6.9 TB/s; to bf16 52 us, 6.7 TB/s)
 constexpr int SEG = 4096;
 
 template <bool BF16>

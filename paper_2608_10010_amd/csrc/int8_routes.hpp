@@ -56,10 +56,10 @@ inline bool turned(int64_t M, int64_t N, int64_t K) {
 
 // Slot by slot or expert by expert, by estimated time in us: three launches and their latencies, the weights of the
 // experts that T tokens take on average at 5.4 TB/s and those that slots share at 6.5, or 6 us for each 512
-// workgroups, which rank E logits first; or five launches and the experts' weights at 5.2 TB/s (fp32: 4.6).  (1 token, 8
-// of 64 experts of 2048 x 1024: 18 us against 40; 4 tokens 46 against 52; 12 tokens, 4 of 128 60 against 74; 16 tokens, 8
-// of 128 of 2048 x 768 107 against 102; 64 tokens, 2 of 16 103 against 45; fp32, 7 tokens, 2 of 16 of 4096 x 2048 68
-// against 77.)
+// workgroups of 32 columns, which rank E logits first (fp32's workgroups have 16 columns and take half as long); or five
+// launches and the experts' weights at 5.2 TB/s (fp32: 4.6).  (1 token, 8 of 64 experts of 2048 x 1024: 18 us against 40; 4
+// tokens 46 against 52; 12 tokens, 4 of 128 60 against 74; 16 tokens, 8 of 128 of 2048 x 768 107 against 102; 64 tokens, 2
+// of 16 103 against 45; fp32, 7 tokens, 2 of 16 of 4096 x 2048 68 against 77.)
 template <int P>
 inline bool by_slots(int64_t T, int64_t E, int64_t k, int64_t H, int64_t I) {
     if (E > RANKED_EXPERTS) return false;
