@@ -63,3 +63,18 @@ def test_inner_values_far_from_one(T, E, topk, H, I, dtype, k):
     up = gus.copy()
     up[:, I:] = moved(gus[:, I:], k)
     same(i8.cfint8_moe(*dev(x, r, gu, up, dn, moved(dns, -k)), topk), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,E,topk,H,I", SIZES)
+def test_subnormal_activations(T, E, topk, H, I, dtype):
+    """x of whole numbers times 2^-133, every one of them subnormal, against the whole numbers themselves: the 2^133 lies
+    in the router and the gate/up scales."""
+    say(f"[int8 moe] subnormal x T={T} E={E} {dtype}")
+    x, r, gu, gus, dn, dns = make(T, E, H, I, dtype)
+    x = torch.from_numpy(np.random.default_rng(T).integers(-63, 64, (T, H)).astype(np.float32)).to(x.dtype)
+    r[r.abs() < 2.0 ** -10] = 0
+    low = dev(x, moved(r, -30), gu, moved(gus, -30), dn, dns)
+    tiny = torch.from_numpy(np.ldexp(x.float().numpy(), -133)).to(x.dtype)
+    assert float(tiny.abs().max()) < 2.0 ** -126 and torch.equal(tiny.double() * 2.0 ** 133, x.double())
+    same(i8.cfint8_moe(*dev(tiny, moved(r, 103), gu, moved(gus, 103), dn, dns), topk), i8.cfint8_moe(*low, topk))
